@@ -34,6 +34,7 @@
 #ifndef ASD_H
 #define ASD_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #if defined(__GNUC__)
@@ -262,6 +263,123 @@ ASD_API int32_t asd_last_round_count(const asd_ctx* ctx);
  *   kernels a batched verify call of n rows takes (which depend on n as well).
  *   x, out DEV fp32 [n, d]; tau DEV int32 [n]. */
 ASD_API asd_status asd_denoise(asd_ctx* ctx, const float* x, const int32_t* tau, int32_t n, float* out, void* stream);
+
+/* ---- operators of a gated residual network ----------------------------------
+ * What a block  h += W_down (act(W_gate n) * (W_up n)),  n = RMSNorm(h) gain,  is made of, on its own: for 16-bit numbers and,
+ * in forward passes, for 8-bit integers with scales.  They need no asd_ctx.
+ *
+ *  - Matrices are row-major; ld_* are elements between rows (>= the row's length).  Rows, sizes and pitches may be odd;
+ *    pointers are aligned to their element.  rows may be 0 (nothing is done); other sizes are at least 1.
+ *  - All pointers but the structs themselves are DEV, of the device that is current; the call is asynchronous on `stream`,
+ *    allocates nothing and may be captured into a graph.  Outputs must not overlap inputs or each other, except where said.
+ *  - `workspace` (16-byte aligned, workspace_bytes long; what it holds before does not matter) is the caller's, and one call's
+ *    until that call's work on the stream is over: calls on different streams, or graphs that may run at the same time, need
+ *    their own.  asd_*_workspace(args) says how many bytes a call with these sizes, types, pitches and pointers needs; 0: none,
+ *    workspace may be NULL.  (Forward products need one only where rows start at no multiple of 16 bytes.)
+ *  - rows_used (DEV int32 [1], or NULL): where only the device knows how many of the rows there are.  Rows *rows_used .. rows - 1
+ *    of the outputs are left as they were.
+ *  - A row's results depend on that row (and the call's sizes) only, and are the same bits every time. */
+typedef enum { ASD_F32 = 0, ASD_BF16 = 1, ASD_F16 = 2, ASD_I8 = 3 } asd_type;
+typedef enum { ASD_ACT_SILU = 0, ASD_ACT_GELU = 1 /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */ } asd_act;
+
+/* asd_rms_norm: r = x + residual (in fp32; residual may be NULL: r = x); sum = r in x's type (NULL: not wanted; may be x or
+ *   residual itself, with its pitch); and with rstd = (mean of r^2 + eps)^(-1/2), of r before it is rounded:
+ *   out_type ASD_F32, ASD_BF16, ASD_F16: out = r rstd gain.
+ *   out_type ASD_I8: with v = r gain, out = the integer nearest to 127 v / max |v| of the row (ties to even) and
+ *   scale[row] (fp32) = max |v| rstd / 127: out * scale is r rstd gain to half a step.  A row of zeros has scale 0; a row that
+ *   holds an infinity or a NaN has scale NaN and integers 0.
+ *   type (of x, residual, sum, gain): ASD_F32, ASD_BF16 or ASD_F16.  gain [cols], or NULL: 1.  cols <= 65536.
+ * asd_quantize_rows: the same without sum and norm: out (int8) = nearest integer to 127 x / max |x|, scale = max |x| / 127.
+ *   Uses rows, cols, type, x, ld_x, out, ld_out, scale, rows_used; ignores the other fields. */
+typedef struct {
+  int32_t rows, cols;
+  int32_t type, out_type; /* asd_type */
+  const void* x;
+  const void* residual;
+  const void* gain;
+  void* sum;
+  void* out;
+  float* scale;
+  int64_t ld_x, ld_residual, ld_sum, ld_out;
+  double eps; /* >= 0 */
+  const int32_t* rows_used;
+} asd_norm;
+ASD_API asd_status asd_rms_norm(const asd_norm* p, void* stream);
+ASD_API asd_status asd_quantize_rows(const asd_norm* p, void* stream);
+
+/* asd_rms_norm_backward: gradients of out = r rstd gain (numbers), from dy, the gradient of out, and sum, the r of the forward
+ *   pass as it was stored:  n = r rstd,  dx = rstd (gain dy - n mean(gain dy n)) + dsum,  dgain = sum over rows of dy n.
+ *   dx is the gradient of x and of residual alike; dsum (NULL: 0) the gradient that reaches sum from elsewhere.  dx (NULL: not
+ *   wanted) may be dy or dsum itself, with its pitch; dgain [cols] in `type` (NULL: not wanted; gain NULL: 1). */
+typedef struct {
+  int32_t rows, cols;
+  int32_t type;
+  const void* dy;
+  const void* sum;
+  const void* gain;
+  const void* dsum;
+  void* dx;
+  void* dgain;
+  int64_t ld_dy, ld_sum, ld_dsum, ld_dx;
+  double eps;
+  void* workspace;
+  size_t workspace_bytes;
+} asd_norm_grad;
+ASD_API size_t asd_rms_norm_backward_workspace(const asd_norm_grad* p);
+ASD_API asd_status asd_rms_norm_backward(const asd_norm_grad* p, void* stream);
+
+/* asd_linear_i8: out[m][n] = (sum over k of x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n]:  x int8 [rows, cols] with a scale
+ *   per row, w int8 [channels, cols] with a scale per channel (scales and bias fp32; bias may be NULL).  Sums are exact (32-bit
+ *   integers; cols <= 131071).  out_type ASD_F32, ASD_BF16 or ASD_F16, rounded once. */
+typedef struct {
+  int32_t rows, cols, channels;
+  int32_t out_type;
+  const int8_t* x;
+  const float* x_scale;
+  const int8_t* w;
+  const float* w_scale;
+  const float* bias;
+  void* out;
+  int64_t ld_x, ld_w, ld_out;
+  const int32_t* rows_used;
+  void* workspace;
+  size_t workspace_bytes;
+} asd_linear8;
+ASD_API size_t asd_linear_i8_workspace(const asd_linear8* p);
+ASD_API asd_status asd_linear_i8(const asd_linear8* p, void* stream);
+
+/* asd_gated_ff: out[m][n] = act(g) u,  g = sum over k of x[m][k] w_gate[n][k],  u the same with w_up: both projections, the
+ *   activation and the product in one pass, nothing but out written.  Sums, activation and product in fp32, rounded once.
+ *   type ASD_BF16, ASD_F16: x, the weights and out (out_type == type); the scales are not used.
+ *   type ASD_I8: g and u as asd_linear_i8 has them, without bias; out_type ASD_BF16 or ASD_F16; cols <= 131071.
+ * asd_gated_ff_backward: from dh [rows, channels], the gradient of out (ASD_BF16, ASD_F16; pitch ld_dh), with
+ *   dg = dh u act'(g), du = dh act(g) (g, u computed again, in fp32; dg, du rounded to `type` for the products):
+ *   dx = dg W_gate + du W_up [rows, cols],  dw_gate = dg^T x,  dw_up = du^T x [channels, cols], all in `type`.  dx may be NULL,
+ *   and dw_gate and dw_up may both be.  rows 0: the weights' gradients are zero.  rows_used must be NULL. */
+typedef struct {
+  int32_t rows, cols, channels;
+  int32_t type, out_type, act; /* asd_type, asd_act */
+  const void* x;
+  const float* x_scale;
+  const void* w_gate;
+  const void* w_up;
+  const float* gate_scale;
+  const float* up_scale;
+  void* out;
+  int64_t ld_x, ld_w_gate, ld_w_up, ld_out;
+  const int32_t* rows_used;
+  const void* dh;
+  void* dx;
+  void* dw_gate;
+  void* dw_up;
+  int64_t ld_dh, ld_dx, ld_dw_gate, ld_dw_up;
+  void* workspace;
+  size_t workspace_bytes;
+} asd_gated;
+ASD_API size_t asd_gated_ff_workspace(const asd_gated* p);
+ASD_API asd_status asd_gated_ff(const asd_gated* p, void* stream);
+ASD_API size_t asd_gated_ff_backward_workspace(const asd_gated* p);
+ASD_API asd_status asd_gated_ff_backward(const asd_gated* p, void* stream);
 
 /* ---- host-only helpers -----------------------------------------------------
  * DDPM linear-beta schedule (beta_tau from beta_min to beta_max over tau=1..K)

@@ -13,6 +13,8 @@ LIB_PATH = os.path.join(_HERE, "libasd.so")
 
 ASD_OK, ASD_EINVAL, ASD_ENOMEM, ASD_EDEVICE, ASD_ESTATE, ASD_EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 ASD_DEN_GMM, ASD_DEN_MLP = 1, 2
+ASD_F32, ASD_BF16, ASD_F16, ASD_I8 = 0, 1, 2, 3
+ASD_ACT_SILU, ASD_ACT_GELU = 0, 1
 PROF = dict(MODEL=0, PLAN=1, GMM_ROWWISE=2, GMM_LOGITS=3, GMM_SOFTMAX=4, GMM_COMBINE=5, MLP_PACK=6, MLP_GEMM_IN=7,
             MLP_GEMM_BLK=8, MLP_GEMM_OUT=9, DRAFT=10, ACCEPT=11, GMM_SCREEN=12, GMM_CERT=13, ACCEPT_EARLY=14)
 
@@ -42,6 +44,42 @@ class asd_denoiser(C.Structure):
 class asd_config(C.Structure):
     _fields_ = [("sched", asd_schedule), ("den", asd_denoiser), ("L", C.c_int32), ("chains", C.c_int32),
                 ("seed", C.c_uint64)]
+
+
+class asd_norm(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("type", C.c_int32), ("out_type", C.c_int32),
+                ("x", C.c_void_p), ("residual", C.c_void_p), ("gain", C.c_void_p), ("sum", C.c_void_p),
+                ("out", C.c_void_p), ("scale", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_residual", C.c_int64), ("ld_sum", C.c_int64), ("ld_out", C.c_int64),
+                ("eps", C.c_double), ("rows_used", C.c_void_p)]
+
+
+class asd_norm_grad(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("type", C.c_int32),
+                ("dy", C.c_void_p), ("sum", C.c_void_p), ("gain", C.c_void_p), ("dsum", C.c_void_p),
+                ("dx", C.c_void_p), ("dgain", C.c_void_p),
+                ("ld_dy", C.c_int64), ("ld_sum", C.c_int64), ("ld_dsum", C.c_int64), ("ld_dx", C.c_int64),
+                ("eps", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class asd_linear8(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("channels", C.c_int32), ("out_type", C.c_int32),
+                ("x", C.c_void_p), ("x_scale", C.c_void_p), ("w", C.c_void_p), ("w_scale", C.c_void_p),
+                ("bias", C.c_void_p), ("out", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_w", C.c_int64), ("ld_out", C.c_int64), ("rows_used", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class asd_gated(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("channels", C.c_int32),
+                ("type", C.c_int32), ("out_type", C.c_int32), ("act", C.c_int32),
+                ("x", C.c_void_p), ("x_scale", C.c_void_p), ("w_gate", C.c_void_p), ("w_up", C.c_void_p),
+                ("gate_scale", C.c_void_p), ("up_scale", C.c_void_p), ("out", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_w_gate", C.c_int64), ("ld_w_up", C.c_int64), ("ld_out", C.c_int64),
+                ("rows_used", C.c_void_p),
+                ("dh", C.c_void_p), ("dx", C.c_void_p), ("dw_gate", C.c_void_p), ("dw_up", C.c_void_p),
+                ("ld_dh", C.c_int64), ("ld_dx", C.c_int64), ("ld_dw_gate", C.c_int64), ("ld_dw_up", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 _lib = None
@@ -94,6 +132,16 @@ def lib():
             "asd_profile_accept_rows": (i32, [vp, vp, vp]),
             "asd_debug_philox": (i32, [u64, u32, u32, u32, i32, vp, vp]),
             "asd_debug_randoms": (i32, [u64, u32, u32, i32, vp, vp, vp]),
+            "asd_rms_norm": (i32, [C.POINTER(asd_norm), vp]),
+            "asd_quantize_rows": (i32, [C.POINTER(asd_norm), vp]),
+            "asd_rms_norm_backward_workspace": (C.c_size_t, [C.POINTER(asd_norm_grad)]),
+            "asd_rms_norm_backward": (i32, [C.POINTER(asd_norm_grad), vp]),
+            "asd_linear_i8_workspace": (C.c_size_t, [C.POINTER(asd_linear8)]),
+            "asd_linear_i8": (i32, [C.POINTER(asd_linear8), vp]),
+            "asd_gated_ff_workspace": (C.c_size_t, [C.POINTER(asd_gated)]),
+            "asd_gated_ff": (i32, [C.POINTER(asd_gated), vp]),
+            "asd_gated_ff_backward_workspace": (C.c_size_t, [C.POINTER(asd_gated)]),
+            "asd_gated_ff_backward": (i32, [C.POINTER(asd_gated), vp]),
             "asd_schedule_ddpm_linear": (i32, [i32, C.c_double, C.c_double, vp, vp, vp, vp, vp]),
             "asd_schedule_from_abar": (i32, [i32, vp, vp, vp, vp, vp, vp]),
             "asd_abar_cosine": (i32, [i32, C.c_double, C.c_double, vp]),

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libasd.so")
 PROBE_LIB = os.path.join(HERE, "libasd_probe.so")
-SOURCES = ["api.hip", "round.hip", "gmm.hip", "gmm_chain.hip", "mlp.hip"]
+SOURCES = ["api.hip", "round.hip", "gmm.hip", "gmm_chain.hip", "mlp.hip", "ops_norm.hip", "ops_gemm.hip"]
 PROBE_SOURCES = ["probe/ceiling.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",

@@ -31,7 +31,7 @@ void set_error(const char* fmt, ...) {
   va_end(ap);
 }
 
-static asd_status fail(asd_status s, const char* fmt, ...) {
+asd_status fail(asd_status s, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);

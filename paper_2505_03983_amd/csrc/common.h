@@ -15,6 +15,7 @@ namespace asd {
 
 // ---- error plumbing ---------------------------------------------------------
 void set_error(const char* fmt, ...);
+asd_status fail(asd_status s, const char* fmt, ...);   // sets the message, returns s
 
 #define ASD_HIP(...)                                                               \
   do {                                                                             \

@@ -1,0 +1,389 @@
+// Products of row-major operands, out[m][n] = sum_k x[m][k] w[n][k], for the operators (ops_gemm.hip): 16-bit numbers with
+// fp32 sums, or 8-bit integers with 32-bit sums.  Both operands are read as they lie in the caller's memory (rows at any pitch
+// that keeps them on 16 bytes; others are copied first): nothing is laid out ahead, so weights that change every training step
+// cost nothing extra.
+//
+// All element types share one geometry, counted in bytes of k: a matrix instruction takes 16 bytes a lane of each operand
+// (8 numbers of 16 bits, 16 integers of 8), 32 bytes of k for 32 rows, and runs for as many cycles with either.
+//
+// The channels' fragment goes in as the instruction's first operand, the rows' as its second: a lane then holds four
+// neighbouring channels of one row in four neighbouring registers, which is what the epilogues store.
+//
+// Gated products (GATED): the tile's channels are groups of 32 of one weight matrix and the same 32 of the other, in turn, so
+// that a wavefront's registers hold both factors of an output element, and the activation and the product are formed there.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "gemm_bf16.h"
+
+namespace asd {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef float v4f_b __attribute__((ext_vector_type(4)));
+
+// Matrix instructions and sums by element type.
+struct ElemBf16 {
+  typedef v16f_b Acc32;
+  typedef v4f_b Acc16;
+  typedef float Sum;
+  static constexpr int kBytes = 2;
+  static __device__ __forceinline__ Acc32 mma32(v4i_b a, v4i_b b, Acc32 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ Acc16 mma16(v4i_b a, v4i_b b, Acc16 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  }
+};
+struct ElemF16 {
+  typedef v16f_b Acc32;
+  typedef v4f_b Acc16;
+  typedef float Sum;
+  static constexpr int kBytes = 2;
+  static __device__ __forceinline__ Acc32 mma32(v4i_b a, v4i_b b, Acc32 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ Acc16 mma16(v4i_b a, v4i_b b, Acc16 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+};
+struct ElemI8 {
+  typedef v16i_b Acc32;
+  typedef v4i_b Acc16;
+  typedef int Sum;
+  static constexpr int kBytes = 1;
+  static __device__ __forceinline__ Acc32 mma32(v4i_b a, v4i_b b, Acc32 c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ Acc16 mma16(v4i_b a, v4i_b b, Acc16 c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+};
+
+// Rows of x and of one or two weight matrices (w1 NULL: one); pitches and kb, the bytes of a row, are multiples of 16, and so are
+// the pointers.
+struct RowsProduct {
+  const uint8_t* x;
+  const uint8_t* w0;
+  const uint8_t* w1;
+  int64_t x_pitch, w_pitch0, w_pitch1;   // bytes between rows
+  int M, N;                              // rows; channels (of one weight matrix)
+  int64_t kb;
+  const int32_t* rows_used;              // DEV or NULL: rows to work on where the host knows a bound, M, only
+};
+
+// BM x BN workgroup tile (BN counts both matrices' channels in a gated product), WGM x WGN wavefronts, BKB bytes of k per stage.
+template <int BM_, int BN_, int WGM_, int WGN_, int BKB_, int STAGES_>
+struct RowsCfg {
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, BKB = BKB_, STAGES = STAGES_;
+  static constexpr int NW = WGM * WGN, THREADS = 64 * NW;
+  static constexpr int WM = BM / WGM, WN = BN / WGN, MI = WM / 32, NJ = WN / 32;
+  static constexpr int RPL = 1024 / BKB;                              // rows a wavefront's load of 1 KB covers
+  static constexpr int X_LOADS = BM / RPL / NW, W_LOADS = BN / RPL / NW, LPS = X_LOADS + W_LOADS;
+  static constexpr int STAGE_BYTES = (BM + BN) * BKB, NG = BKB / 32;  // groups of 32 bytes of k per stage
+  static constexpr int PIPE_BYTES = STAGES * STAGE_BYTES;
+  static_assert(WM % 32 == 0 && WN % 32 == 0 && STAGES >= 2 && (BKB == 64 || BKB == 128), "tile shape");
+  static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0, "loads must divide evenly among the wavefronts");
+  static_assert(PIPE_BYTES <= 160 * 1024 && LPS * (STAGES - 1) <= 63, "LDS of a CU, vmcnt range");
+};
+
+// Wait until at most `stages` * LPS of this wavefront's loads are outstanding.
+template <int LPS, int MAX>
+__device__ __forceinline__ void wait_rows_stages(int stages) {
+  if constexpr (MAX == 0) {
+    wait_vmcnt<0>();
+  } else {
+    if (stages >= MAX) wait_vmcnt<LPS * MAX>();
+    else wait_rows_stages<LPS, MAX - 1>(stages);
+  }
+}
+
+// As load_to_lds, with a scalar part of the offset.
+__device__ __forceinline__ void load_rows_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t off, uint32_t k, void* dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)dst, 16, (int)off, (int)k, 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, -1, 0x00027000);
+}
+
+// Tile of a workgroup.  Workgroups go to the XCDs in turn; each XCD takes a run of consecutive tiles, which go down kGroupRows
+// row tiles before they go right, so that the 32 tiles an XCD works on at a time share operands in its L2.
+constexpr int kGroupRows = 8;
+__device__ __forceinline__ bool rows_tile(int tiles_m, int tiles_n, int* tm, int* tn) {
+  const int total = tiles_m * tiles_n, per_xcd = (total + 7) / 8;
+  const int lin = blockIdx.x, xcd = lin & 7, at = lin >> 3;
+  const int full = total - 8 * (per_xcd - 1);          // XCDs with per_xcd tiles; the others have one less
+  const int id = xcd < full ? xcd * per_xcd + at : full * per_xcd + (xcd - full) * (per_xcd - 1) + at;
+  if (at >= (xcd < full ? per_xcd : per_xcd - 1)) return false;
+  const int group = id / (kGroupRows * tiles_n), rest = id - group * kGroupRows * tiles_n;
+  const int high = min(kGroupRows, tiles_m - group * kGroupRows);
+  *tm = group * kGroupRows + rest % high;
+  *tn = rest / high;
+  return true;
+}
+
+template <class E, class Cfg, class Epi>
+__global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
+  constexpr bool GATED = Epi::kGated;
+  constexpr int BM = Cfg::BM, BN = Cfg::BN, MI = Cfg::MI, NJ = Cfg::NJ, BKB = Cfg::BKB, STAGES = Cfg::STAGES, NG = Cfg::NG;
+  constexpr int X_LOADS = Cfg::X_LOADS, W_LOADS = Cfg::W_LOADS, LPS = Cfg::LPS, NW = Cfg::NW, RPL = Cfg::RPL;
+  constexpr int CPR = BKB / 16;                       // chunks of 16 bytes per row of a stage
+  static_assert(!GATED || NJ % 2 == 0, "both factors in one wavefront");
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
+
+  int tm, tn;
+  if (!rows_tile(tiles_m, tiles_n, &tm, &tn)) return;
+  const int M = p.rows_used ? min(max(*p.rows_used, 0), p.M) : p.M;
+  const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
+  if (m0 >= M) return;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / Cfg::WGN, wn = wave % Cfg::WGN;
+  const int l32 = lane & 31, half = lane >> 5;
+
+  // LDS: a stage holds the tile's rows of x, then of the weights, BKB bytes each.  Chunk c of row r lies in slot
+  // c ^ key(r), so that the 32 rows of a fragment read spread over all banks; the permutation is applied on the global side of
+  // the loads, inside a row's own BKB bytes.
+  constexpr int KEY_SHIFT = BKB == 128 ? 1 : 2;
+  auto key_of = [](int row) { return (row >> KEY_SHIFT) & (CPR - 1); };
+  const __amdgpu_buffer_rsrc_t xr = rows_rsrc(p.x + (int64_t)m0 * p.x_pitch);
+  const __amdgpu_buffer_rsrc_t w0r = rows_rsrc(p.w0 + (int64_t)n0 * p.w_pitch0);
+  const __amdgpu_buffer_rsrc_t w1r = rows_rsrc(GATED ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0);
+  uint32_t x_off[X_LOADS], w_off[W_LOADS];
+  const int sub_row = lane / CPR, slot = lane % CPR;
+#pragma unroll
+  for (int i = 0; i < X_LOADS; ++i) {                 // (rows past the last repeat it; their results are not stored)
+    const int row = (wave + NW * i) * RPL + sub_row;
+    x_off[i] = (uint32_t)((int64_t)min(row, M - 1 - m0) * p.x_pitch) + (uint32_t)((slot ^ key_of(row)) * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < W_LOADS; ++i) {
+    const int row = (wave + NW * i) * RPL + sub_row;
+    const int ch = GATED ? (row >> 6) * 32 + (row & 31) : row;
+    const int64_t pitch = GATED && ((row >> 5) & 1) ? p.w_pitch1 : p.w_pitch0;
+    w_off[i] = (uint32_t)((int64_t)min(ch, p.N - 1 - n0) * pitch) + (uint32_t)((slot ^ key_of(row)) * 16);
+  }
+  auto second = [&](int i) { return GATED && (((wave + NW * i) * RPL >> 5) & 1); };   // the wavefront's load i is of w1
+
+  // k runs over whole stages; what is left of it over BKB comes first, through registers and filled with zeros.
+  const int rest = (int)(p.kb % BKB), nk = (int)(p.kb / BKB) + (rest ? 1 : 0);
+  const uint32_t k_first = rest ? (uint32_t)rest : 0u;   // the first stage that is loaded directly starts here: stage s at
+  auto k_of = [&](int s) { return (uint32_t)(rest ? (s - 1) * BKB + (int)k_first : s * BKB); };
+  auto issue = [&](int s, uint8_t* sb, int first, int count) {
+    const uint32_t k = k_of(s);
+#pragma unroll
+    for (int q = 0; q < LPS; ++q) {
+      if (q < first || q >= first + count) continue;
+      if (q < X_LOADS) load_rows_to_lds(xr, x_off[q], k, sb + (wave + NW * q) * 1024);
+      else load_rows_to_lds(second(q - X_LOADS) ? w1r : w0r, w_off[q - X_LOADS], k, sb + BM * BKB + (wave + NW * (q - X_LOADS)) * 1024);
+    }
+  };
+
+  typename E::Acc32 acc[NJ][MI];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[j][i][r] = 0;
+
+  if (rest) {
+#pragma unroll
+    for (int q = 0; q < LPS; ++q) {
+      const int b = q < X_LOADS ? wave + NW * q : wave + NW * (q - X_LOADS);
+      const int at = (slot ^ key_of(b * RPL + sub_row)) * 16;
+      const uint8_t* base = q < X_LOADS ? p.x + (int64_t)m0 * p.x_pitch
+                            : second(q - X_LOADS) ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0;
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (at < rest) v = *reinterpret_cast<const uint4*>(base + (q < X_LOADS ? x_off[q < X_LOADS ? q : 0] : w_off[q < X_LOADS ? 0 : q - X_LOADS]));
+      *reinterpret_cast<uint4*>(rows_lds + (q < X_LOADS ? 0 : BM * BKB) + b * 1024 + lane * 16) = v;
+    }
+  } else if (nk > 0) {
+    issue(0, rows_lds, 0, LPS);
+  }
+#pragma unroll
+  for (int s = 1; s < STAGES - 1; ++s)
+    if (s < nk) issue(s, rows_lds + s * Cfg::STAGE_BYTES, 0, LPS);
+
+  v4i_b xf[2][MI], wf[2][NJ];
+  const int x_row = (wm * Cfg::WM + l32) * BKB, w_row = BM * BKB + (wn * Cfg::WN + l32) * BKB;
+  int cp[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) cp[g] = ((2 * g + half) ^ key_of(l32)) * 16;   // (tile offsets are multiples of 32: same keys)
+  auto read_frags = [&](const uint8_t* sb, int g, int buf) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) wf[buf][j] = *reinterpret_cast<const v4i_b*>(sb + w_row + j * 32 * BKB + cp[g]);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) xf[buf][i] = *reinterpret_cast<const v4i_b*>(sb + x_row + i * 32 * BKB + cp[g]);
+  };
+  constexpr int G = MI * NJ;
+  auto mma = [&](int buf, int first, int count) {
+#pragma unroll
+    for (int q = 0; q < G; ++q)
+      if (q >= first && q < first + count) acc[q % NJ][q / NJ] = E::mma32(wf[buf][q % NJ], xf[buf][q / NJ], acc[q % NJ][q / NJ]);
+  };
+
+  // ---- pipeline: everything that is not a matrix instruction runs in the shadow of one (as in gemm_bf16_slab.h).  Each group's
+  // instructions have the next group's fragment reads and a share of the loads of stage kt + STAGES - 1 slotted in; half-way
+  // through a stage's last group the wavefront waits for its loads of the next stage, meets the others and reads on there.
+  constexpr int H1 = (G + 1) / 2, H2 = G - H1, RD = MI + NJ, SLOTS = (RD + 1) / 2, RLAST = RD - 2 * (SLOTS - 1);
+  constexpr int REM = G > SLOTS ? G - SLOTS : 0;
+  constexpr int LPG = (LPS + NG - 1) / NG;
+  if (nk > 0) {
+    wait_rows_stages<LPS, STAGES - 2>(nk - 1);
+    lds_handover();
+    read_frags(rows_lds, 0, 0);
+  }
+  int cur = 0, nst = STAGES - 1;
+  auto step = [&](int kt, auto steady_c) {
+    constexpr bool steady = decltype(steady_c)::value;
+    const uint8_t* sb = rows_lds + cur * Cfg::STAGE_BYTES;
+    uint8_t* nb = rows_lds + nst * Cfg::STAGE_BYTES;
+    const int nxt = kt + STAGES - 1;
+    nst = cur;
+    cur = cur + 1 == STAGES ? 0 : cur + 1;
+#pragma unroll
+    for (int g = 0; g < NG - 1; ++g) {
+      read_frags(sb, g + 1, (g + 1) & 1);
+      if constexpr (steady) issue(nxt, nb, g * LPG, LPG);
+      mma(g & 1, 0, G);
+      sched_pairs<0x100, (SLOTS - 1 < G ? SLOTS - 1 : G), 2>();
+      if constexpr (SLOTS <= G) sched_pairs<0x100, 1, RLAST>();
+      sched_pairs<0x010, (LPG < REM ? LPG : REM), 1>();
+      sched_mfma<REM - (LPG < REM ? LPG : REM)>();
+    }
+    if constexpr (steady) issue(nxt, nb, (NG - 1) * LPG, LPG);
+    mma((NG - 1) & 1, 0, H1);
+    sched_pairs<0x010, (LPG < H1 ? LPG : H1), 1>();
+    sched_mfma<H1 - (LPG < H1 ? LPG : H1)>();
+    if (steady || kt + 1 < nk) {
+      if constexpr (steady) wait_vmcnt<LPS * (STAGES - 2)>();
+      else wait_rows_stages<LPS, STAGES - 2>(nk - 2 - kt);
+      lds_handover();
+      read_frags(rows_lds + cur * Cfg::STAGE_BYTES, 0, 0);
+    }
+    mma((NG - 1) & 1, H1, H2);
+    sched_pairs<0x100, (SLOTS - 1 < H2 ? SLOTS - 1 : H2), 2>();
+  };
+  static_assert(NG % 2 == 0, "a stage's first group is in the first buffer");
+  int kt = 0;
+  for (; kt + STAGES - 1 < nk; ++kt) step(kt, std::true_type());
+  for (; kt < nk; ++kt) step(kt, std::false_type());
+
+  // ---- epilogue.  A lane holds, for each of its MI rows, four channels at 8 q + 4 half of each group of 32.  The results go
+  // through LDS (the stages are free) in the output's type, 64 columns a wavefront or 32 where two factors become one, so
+  // that rows leave in whole runs; LDS slots of 16 bytes are permuted by the row for the banks.
+  lds_handover();
+  typedef typename Epi::Out Out;
+  constexpr int COLS = Cfg::WN / (GATED ? 2 : 1), OB = (int)sizeof(Out);
+  constexpr int ROWB = COLS * OB, SL = ROWB / 16;           // bytes and slots of a row
+  constexpr int ROWS = 32;                                  // rows parked at a time: one row group
+  static_assert(NW * ROWS * ROWB <= Cfg::PIPE_BYTES, "parked results");
+  static_assert(SL >= 2 && SL <= 64 && (SL & (SL - 1)) == 0, "slots of a parked row");
+  uint8_t* park = rows_lds + wave * (ROWS * ROWB);
+  const int col0 = n0 + wn * COLS;                          // channel of the wavefront's first column
+  for (int out = 0; out < Epi::kOutputs; ++out) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int mrow = m0 + wm * Cfg::WM + i * 32;
+      if (mrow >= M) break;
+      const int m = min(mrow + l32, M - 1);
+      const auto rc = epi.row(m);
+#pragma unroll
+      for (int j = 0; j < NJ; j += GATED ? 2 : 1)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = (GATED ? j / 2 : j) * 32 + 8 * q + 4 * half;
+          typename E::Sum a[4], b[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            a[r] = acc[j][i][4 * q + r];
+            b[r] = acc[GATED ? j + 1 : j][i][4 * q + r];
+          }
+          Out v[4];
+          epi.values(out, rc, m, col0 + c, a, b, v);
+          const int byte = c * OB, sl = (byte >> 4) ^ (l32 & (SL - 1));
+          if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + l32 * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v);
+          else *reinterpret_cast<uint4*>(park + l32 * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v);
+        }
+      // (the region is this wavefront's own, whose LDS operations complete in order)
+      constexpr int RPI = 64 / SL;                          // rows a pass of the wavefront covers
+#pragma unroll
+      for (int r0 = 0; r0 < ROWS; r0 += RPI) {
+        const int r = r0 + lane / SL, sl = lane % SL;
+        const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
+        if (mrow + r < M) epi.store(out, mrow + r, col0 + sl * (16 / OB), v);
+      }
+    }
+  }
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+// Up to 64 rows: a stream of the weights.  A workgroup of eight wavefronts owns 16 channels (of each matrix) and all rows; the
+// wavefronts take 128 bytes of k in turn, straight from memory into the matrix instructions' operands (an instruction takes
+// 64 bytes of 16 rows), kDepth such pieces in flight, and the eight partial sums meet in LDS.  Sums are added in the order of
+// the wavefronts: the same bits every time, and for any number of rows.
+template <class E, int MT, class Epi>
+__global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi epi) {
+  constexpr bool GATED = Epi::kGated;
+  constexpr int WT = GATED ? 2 : 1, NWAVES = 8, DEPTH = MT == 1 ? 4 : 2;
+  const int M = p.rows_used ? min(max(*p.rows_used, 0), p.M) : p.M;
+  const int m0 = blockIdx.y * (16 * MT), n0 = blockIdx.x * 16;
+  if (m0 >= M) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
+  const uint8_t* wrow[WT];
+  wrow[0] = p.w0 + (int64_t)min(n0 + l16, p.N - 1) * p.w_pitch0;
+  if constexpr (GATED) wrow[1] = p.w1 + (int64_t)min(n0 + l16, p.N - 1) * p.w_pitch1;
+  const uint8_t* xrow[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) xrow[i] = p.x + (int64_t)min(m0 + i * 16 + l16, M - 1) * p.x_pitch;
+  typename E::Acc16 acc[WT][MT];
+#pragma unroll
+  for (int t = 0; t < WT; ++t)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[t][i][r] = 0;
+  const v4i_b zero = {0, 0, 0, 0};
+  for (int64_t k0 = (int64_t)wave * 128; k0 < p.kb; k0 += (int64_t)NWAVES * 128 * DEPTH) {
+    v4i_b wf[DEPTH][2][WT], xf[DEPTH][2][MT];
+#pragma unroll
+    for (int s = 0; s < DEPTH; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t k = k0 + (int64_t)s * NWAVES * 128 + h * 64 + quarter * 16;
+        const bool in = k < p.kb;
+#pragma unroll
+        for (int t = 0; t < WT; ++t) wf[s][h][t] = in ? __builtin_nontemporal_load(reinterpret_cast<const v4i_b*>(wrow[t] + k)) : zero;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xf[s][h][i] = in ? *reinterpret_cast<const v4i_b*>(xrow[i] + k) : zero;
+      }
+#pragma unroll
+    for (int s = 0; s < DEPTH; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < WT; ++t)
+#pragma unroll
+          for (int i = 0; i < MT; ++i) acc[t][i] = E::mma16(wf[s][h][t], xf[s][h][i], acc[t][i]);
+  }
+  // lane: row l16, channels 4 quarter .. + 3
+  __shared__ __attribute__((aligned(16))) typename E::Sum part[NWAVES][WT][MT][16][16];
+#pragma unroll
+  for (int t = 0; t < WT; ++t)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<typename E::Acc16*>(&part[wave][t][i][l16][4 * quarter]) = acc[t][i];
+  __syncthreads();
+  for (int e = tid; e < MT * 256; e += 512) {
+    const int i = e >> 8, row = (e >> 4) & 15, c = e & 15, m = m0 + i * 16 + row, n = n0 + c;
+    if (m >= M || n >= p.N) continue;
+    typename E::Sum a = part[0][0][i][row][c], b = part[0][WT - 1][i][row][c];
+#pragma unroll
+    for (int w = 1; w < NWAVES; ++w) {
+      a += part[w][0][i][row][c];
+      if constexpr (GATED) b += part[w][1][i][row][c];
+    }
+    epi.one(m, n, a, b);
+  }
+}
+
+}  // namespace asd

@@ -1,0 +1,54 @@
+// Shared by the operators' C entries (ops_norm.hip, ops_gemm.hip): argument checks and element types.
+#pragma once
+#include "common.h"
+
+namespace asd {
+
+inline int type_bytes(int t) { return t == ASD_F32 ? 4 : t == ASD_BF16 || t == ASD_F16 ? 2 : t == ASD_I8 ? 1 : 0; }
+inline bool float_type(int t) { return t == ASD_F32 || t == ASD_BF16 || t == ASD_F16; }
+inline bool half_type(int t) { return t == ASD_BF16 || t == ASD_F16; }
+
+// A matrix argument: `rows` rows of `cols` elements of `bytes`, `ld` elements apart.
+struct MatArg {
+  const char* name;
+  const void* p;
+  int64_t rows, cols, ld;
+  int bytes;
+  bool out;
+  const char* begin() const { return static_cast<const char*>(p); }
+  const char* end() const { return begin() + ((rows - 1) * ld + cols) * bytes; }
+};
+
+// Pitches, alignment and overlaps of a call's matrices (NULL ones are left out).  may_share(a, b): an output and an input that
+// may be the same array.
+template <class Share>
+inline asd_status check_mats(const MatArg* m, int n, Share may_share) {
+  for (int i = 0; i < n; ++i) {
+    if (!m[i].p || m[i].rows < 1) continue;
+    if (m[i].ld < m[i].cols) return fail(ASD_EINVAL, "ld of %s is below its row length", m[i].name);
+    if (m[i].rows > 1 && m[i].ld > ((int64_t)1 << 40) / m[i].rows) return fail(ASD_EINVAL, "ld of %s is out of range", m[i].name);
+    if ((uintptr_t)m[i].p % m[i].bytes) return fail(ASD_EINVAL, "%s is not aligned to its elements", m[i].name);
+  }
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j) {
+      if (i == j || !m[i].out || !m[i].p || !m[j].p || m[i].rows < 1 || m[j].rows < 1 || (m[j].out && j < i)) continue;
+      if (m[i].begin() >= m[j].end() || m[j].begin() >= m[i].end()) continue;
+      if (may_share(i, j) && m[i].p == m[j].p && (m[i].ld == m[j].ld || m[i].rows == 1)) continue;
+      return fail(ASD_EINVAL, "%s overlaps %s", m[i].name, m[j].name);
+    }
+  return ASD_OK;
+}
+inline asd_status check_mats(const MatArg* m, int n) {
+  return check_mats(m, n, [](int, int) { return false; });
+}
+
+// Rows at any 16 bytes: what the wide loads and stores ask for.
+inline bool on16(const void* p, int64_t ld, int bytes) { return ((uintptr_t)p & 15) == 0 && (ld * bytes & 15) == 0; }
+
+// For the library's own launches: the operators without their argument checks.
+asd_status launch_rms_norm(const asd_norm& p, hipStream_t st);
+asd_status launch_quantize_rows(const asd_norm& p, hipStream_t st);
+asd_status launch_linear8(const asd_linear8& p, hipStream_t st);
+asd_status launch_gated(const asd_gated& p, hipStream_t st);
+
+}  // namespace asd

@@ -1,0 +1,565 @@
+// The operators that are products: 8-bit linear layer, gated unit and its gradient.  The kernels are in gemm_rows.h; here are
+// their epilogues, the choice of tile, and the passes that bring operands into a form the kernels read (copies of rows that
+// start at no multiple of 16 bytes; the gradient's transposed operands).
+#include <math.h>
+
+#include <atomic>
+
+#include "gemm_rows.h"
+#include "ops.h"
+
+namespace asd {
+
+// ---- epilogues -----------------------------------------------------------------------------------------------------------
+// A run of 16 bytes of results, columns n .. of row m of a matrix with n_cols columns.
+template <class T>
+__device__ __forceinline__ void store_cols(T* row, int n, int n_cols, bool wide, uint4 v) {
+  constexpr int CNT = 16 / (int)sizeof(T);
+  if (wide && n + CNT <= n_cols) {
+    *reinterpret_cast<uint4*>(row + n) = v;
+    return;
+  }
+  T e[CNT];
+  *reinterpret_cast<uint4*>(e) = v;
+#pragma unroll
+  for (int k = 0; k < CNT; ++k)
+    if (n + k < n_cols) row[n + k] = e[k];
+}
+
+// out = sum (a gradient's product); rows from `second` on go to the other output (dw_gate, dw_up as one product)
+template <class T>
+struct SumEpi {
+  T* out;
+  T* out2;
+  int64_t ld, ld2;
+  int N, first_rows, second;   // rows 0 .. first_rows - 1 and second .. second + first_rows - 1 are stored
+  bool wide;
+  typedef T Out;
+  static constexpr bool kGated = false;
+  static constexpr int kOutputs = 1;
+  struct Row {};
+  __device__ __forceinline__ Row row(int) const { return Row{}; }
+  __device__ __forceinline__ void values(int, Row, int, int, const float* a, const float*, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (T)a[r];
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const {
+    if (m < first_rows) store_cols(out + m * ld, n, N, wide, v);
+    else if (m >= second && m < second + first_rows) store_cols(out2 + (m - second) * ld2, n, N, wide, v);
+  }
+  __device__ __forceinline__ void one(int m, int n, float a, float) const {
+    if (m < first_rows) out[m * ld + n] = (T)a;
+    else if (m >= second && m < second + first_rows) out2[(m - second) * ld2 + n] = (T)a;
+  }
+};
+
+// out = sum x_scale w_scale + bias
+template <class T>
+struct Scaled8Epi {
+  T* out;
+  int64_t ld;
+  const float* x_scale;
+  const float* w_scale;
+  const float* bias;   // or NULL
+  int N;
+  bool wide;
+  typedef T Out;
+  static constexpr bool kGated = false;
+  static constexpr int kOutputs = 1;
+  __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
+  __device__ __forceinline__ float value(float xs, int n, int a) const {
+    const float v = (float)a * xs * w_scale[n];
+    return bias ? v + bias[n] : v;
+  }
+  __device__ __forceinline__ void values(int, float xs, int, int n, const int* a, const int*, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (T)value(xs, min(n + r, N - 1), a[r]);
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, wide, v); }
+  __device__ __forceinline__ void one(int m, int n, int a, int) const { out[m * ld + n] = (T)value(x_scale[m], n, a); }
+};
+
+// Activations and their derivatives, in fp32.  exp2 and the reciprocal are the hardware's (1 ulp each): about 1e-6 of the value,
+// far inside a 16-bit result.  An exponential that overflows is infinity, and its reciprocal 0: the limits.
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
+}
+constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;   // sqrt(2 / pi)
+__device__ __forceinline__ float act_value(int act, float z) {
+  // 0.5 (1 + tanh s) = sigmoid(2 s)
+  return z * sigmoid(act == ASD_ACT_SILU ? z : 2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
+}
+__device__ __forceinline__ void act_both(int act, float z, float* value, float* slope) {
+  const float on = sigmoid(act == ASD_ACT_SILU ? z : 2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
+  const float inner = act == ASD_ACT_SILU ? 1.f : 2.f * kGeluC * fmaf(3.f * kGeluA * z, z, 1.f);
+  *value = z * on;
+  // (on (1 - on) is 0 where the sigmoid is saturated, whatever inner grows to)
+  const float bend = on * (1.f - on);
+  *slope = bend > 0.f ? fmaf(z * inner, bend, on) : on;
+}
+
+template <class T>
+struct GatedEpi {
+  T* out;
+  int64_t ld;
+  int N, act;
+  bool wide;
+  typedef T Out;
+  static constexpr bool kGated = true;
+  static constexpr int kOutputs = 1;
+  struct Row {};
+  __device__ __forceinline__ Row row(int) const { return Row{}; }
+  __device__ __forceinline__ void values(int, Row, int, int, const float* g, const float* u, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (T)(act_value(act, g[r]) * u[r]);
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, wide, v); }
+  __device__ __forceinline__ void one(int m, int n, float g, float u) const { out[m * ld + n] = (T)(act_value(act, g) * u); }
+};
+
+template <class T>
+struct Gated8Epi {
+  T* out;
+  int64_t ld;
+  const float* x_scale;
+  const float* gate_scale;
+  const float* up_scale;
+  int N, act;
+  bool wide;
+  typedef T Out;
+  static constexpr bool kGated = true;
+  static constexpr int kOutputs = 1;
+  __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
+  __device__ __forceinline__ T value(float xs, int n, int g, int u) const {
+    return (T)(act_value(act, (float)g * xs * gate_scale[n]) * ((float)u * xs * up_scale[n]));
+  }
+  __device__ __forceinline__ void values(int, float xs, int, int n, const int* g, const int* u, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = value(xs, min(n + r, N - 1), g[r], u[r]);
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, wide, v); }
+  __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(x_scale[m], n, g, u); }
+};
+
+// dg = dh u act'(g) and du = dh act(g), side by side: dgu [rows][2 Np], zeros in the columns N .. Np - 1 of either half.  Rounded
+// to the operands' type, as the products that follow take them.
+template <class T>
+struct GatedGradEpi {
+  T* dgu;
+  int Np;
+  const T* dh;
+  int64_t ld_dh;
+  int N, act;
+  typedef T Out;
+  static constexpr bool kGated = true;
+  static constexpr int kOutputs = 2;
+  struct Row {};
+  __device__ __forceinline__ Row row(int) const { return Row{}; }
+  __device__ __forceinline__ void values(int which, Row, int m, int n, const float* g, const float* u, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float d = n + r < N ? (float)dh[m * ld_dh + n + r] : 0.f;
+      float value, slope;
+      act_both(act, g[r], &value, &slope);
+      v[r] = n + r < N ? (T)(which ? d * value : d * u[r] * slope) : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void store(int which, int m, int n, uint4 v) const {
+    if (n < Np) *reinterpret_cast<uint4*>(dgu + (int64_t)m * 2 * Np + which * Np + n) = v;
+  }
+};
+
+// ---- passes over operands --------------------------------------------------------------------------------------------------
+// Rows of `bytes` bytes at any address and pitch, copied to rows on multiples of 128 bytes, zeros behind them.  Sixteen bytes of
+// the copy a thread.
+__global__ __launch_bounds__(256) void pack_rows_kernel(const uint8_t* __restrict__ src, int64_t pitch, int rows, int64_t bytes,
+                                                        uint8_t* __restrict__ dst, int64_t dst_pitch) {
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16;
+  const int64_t row = at / dst_pitch, k = at - row * dst_pitch;
+  if (row >= rows) return;
+  const uint8_t* s = src + row * pitch + k;
+  uint32_t v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int b = 0; b < 16; ++b)
+    if (k + b < bytes) v[b >> 2] |= (uint32_t)s[b] << (8 * (b & 3));
+  *reinterpret_cast<uint4*>(dst + at) = make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
+// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).
+__global__ __launch_bounds__(256) void transpose16_kernel(const uint16_t* __restrict__ src, int64_t ld, int rows, int cols, int wide,
+                                                          uint16_t* __restrict__ dst, int64_t dst_ld) {
+  __shared__ uint16_t tile[64][72];   // (rows 144 bytes apart: columns of eight rows fall on different banks)
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, t = threadIdx.x;
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+    const int r = pass * 32 + (t >> 3), c = (t & 7) * 8;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (r0 + r < rows) {
+      const uint16_t* s = src + (int64_t)(r0 + r) * ld + c0 + c;
+      if (wide && c0 + c + 8 <= cols) {
+        v = *reinterpret_cast<const uint4*>(s);
+      } else {
+        uint32_t e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c0 + c + k < cols) e[k >> 1] |= (uint32_t)s[k] << (16 * (k & 1));
+        v = make_uint4(e[0], e[1], e[2], e[3]);
+      }
+    }
+    *reinterpret_cast<uint4*>(&tile[r][c]) = v;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+    const int c = pass * 32 + (t >> 3), r = (t & 7) * 8;
+    if (c0 + c >= cols) continue;
+    uint32_t e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e[k >> 1] |= (uint32_t)tile[r + k][c] << (16 * (k & 1));
+    *reinterpret_cast<uint4*>(dst + (int64_t)(c0 + c) * dst_ld + r0 + r) = make_uint4(e[0], e[1], e[2], e[3]);
+  }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------------
+typedef RowsCfg<256, 256, 2, 4, 128, 2> Rows256;
+typedef RowsCfg<128, 128, 2, 2, 128, 2> Rows128;
+typedef RowsCfg<64, 128, 2, 2, 128, 3> Rows64;
+
+template <class E, class Cfg, class Epi>
+static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st) {
+  auto kern = gemm_rows_kernel<E, Cfg, Epi>;
+  static std::atomic<uint64_t> ready{0};   // devices whose limit of dynamic LDS has been raised for this kernel
+  int dev = 0;
+  hipError_t err = hipGetDevice(&dev);
+  if (err != hipSuccess) return err;
+  if (!(ready.load() >> (dev & 63) & 1)) {
+    err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::PIPE_BYTES);
+    if (err != hipSuccess) return err;
+    ready.fetch_or(1ull << (dev & 63));
+  }
+  const int tm = (int)ceil_div(p.M, Cfg::BM), tn = (int)ceil_div(p.N, Epi::kGated ? Cfg::BN / 2 : Cfg::BN);
+  const int64_t grid = ceil_div((int64_t)tm * tn, 8) * 8;
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Cfg::THREADS), Cfg::PIPE_BYTES, st, p, tm, tn, e);
+  return hipGetLastError();
+}
+
+constexpr int kFewRows = 64;
+
+template <class E, class Epi>
+static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st) {
+  if constexpr (Epi::kOutputs == 1) {
+    if (p.M <= kFewRows) {
+      const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
+      const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)ceil_div(p.M, 16 * mt));
+      if (mt == 1) hipLaunchKernelGGL((gemm_few_rows_kernel<E, 1, Epi>), grid, dim3(512), 0, st, p, e);
+      else if (mt == 2) hipLaunchKernelGGL((gemm_few_rows_kernel<E, 2, Epi>), grid, dim3(512), 0, st, p, e);
+      else hipLaunchKernelGGL((gemm_few_rows_kernel<E, 4, Epi>), grid, dim3(512), 0, st, p, e);
+      return hipGetLastError();
+    }
+  }
+  const int64_t n = Epi::kGated ? 2 * (int64_t)p.N : p.N;
+  if (ceil_div(p.M, 256) * ceil_div(n, 256) >= 192) return launch_rows<E, Rows256>(p, e, st);
+  if (ceil_div(p.M, 128) * ceil_div(n, 128) >= 256) return launch_rows<E, Rows128>(p, e, st);
+  return launch_rows<E, Rows64>(p, e, st);
+}
+
+constexpr int64_t kMaxPitch = (int64_t)4 << 20;   // bytes: a tile's offsets stay within 32 bits
+
+// Part of a workspace, in order; bytes are rounded up to 256.
+struct Carve {
+  uint8_t* base;
+  size_t used = 0;
+  uint8_t* take(size_t bytes) {
+    uint8_t* p = base ? base + used : nullptr;
+    used += (bytes + 255) & ~(size_t)255;
+    return p;
+  }
+};
+
+// An operand as the kernels read it: itself, or a copy in the workspace.
+struct Operand {
+  const uint8_t* p;
+  int64_t pitch;   // bytes
+  uint8_t* copy;   // NULL: none
+  const uint8_t* src;
+  int64_t src_pitch;
+  int rows;
+  int64_t bytes;
+};
+static Operand operand(const void* p, int rows, int64_t cols, int64_t ld, int bytes, Carve* ws) {
+  const int64_t row = cols * bytes;
+  if (on16(p, rows > 1 ? ld : 0, bytes) && (row & 15) == 0 && (rows == 1 || ld * bytes <= kMaxPitch))
+    return Operand{static_cast<const uint8_t*>(p), rows > 1 ? ld * bytes : row, nullptr, nullptr, 0, rows, row};
+  const int64_t pitch = ceil_div(row, 128) * 128;
+  uint8_t* c = ws->take((size_t)pitch * rows);
+  return Operand{c, pitch, c ? c : reinterpret_cast<uint8_t*>(1), static_cast<const uint8_t*>(p), ld * bytes, rows, row};
+}
+static hipError_t bring(const Operand& o, hipStream_t st) {
+  if (!o.copy) return hipSuccess;
+  const int64_t threads = o.pitch / 16 * o.rows;
+  hipLaunchKernelGGL(pack_rows_kernel, dim3((unsigned)ceil_div(threads, 256)), dim3(256), 0, st, o.src, o.src_pitch, o.rows, o.bytes, o.copy, o.pitch);
+  return hipGetLastError();
+}
+// Bytes of k the kernels run over: copies have zeros behind their rows.
+static int64_t k_bytes(int64_t row) { return ceil_div(row, 16) * 16; }
+
+// ---- the 8-bit linear layer ----------------------------------------------------------------------------------------------------
+struct Linear8Plan {
+  Operand x, w;
+  size_t bytes;
+};
+static Linear8Plan plan_linear8(const asd_linear8& p, void* ws) {
+  Carve c{static_cast<uint8_t*>(ws)};
+  Linear8Plan r;
+  r.x = operand(p.x, p.rows, p.cols, p.ld_x, 1, &c);
+  r.w = operand(p.w, p.channels, p.cols, p.ld_w, 1, &c);
+  r.bytes = c.used;
+  return r;
+}
+
+template <class T>
+static asd_status run_linear8(const asd_linear8& p, const Linear8Plan& o, hipStream_t st) {
+  const RowsProduct g{o.x.p, o.w.p, nullptr, o.x.pitch, o.w.pitch, 0, p.rows, p.channels, k_bytes(p.cols), p.rows_used};
+  const Scaled8Epi<T> e{static_cast<T*>(p.out), p.ld_out, p.x_scale, p.w_scale, p.bias, p.channels, on16(p.out, p.ld_out, sizeof(T))};
+  ASD_HIP(launch_product<ElemI8>(g, e, st));
+  return ASD_OK;
+}
+
+asd_status launch_linear8(const asd_linear8& p, hipStream_t st) {
+  const Linear8Plan o = plan_linear8(p, p.workspace);
+  ASD_HIP(bring(o.x, st));
+  ASD_HIP(bring(o.w, st));
+  return p.out_type == ASD_F32 ? run_linear8<float>(p, o, st) : p.out_type == ASD_BF16 ? run_linear8<__bf16>(p, o, st) : run_linear8<_Float16>(p, o, st);
+}
+
+// ---- the gated unit --------------------------------------------------------------------------------------------------------------
+struct GatedPlan {
+  Operand x, g, u;
+  size_t bytes;
+};
+static GatedPlan plan_gated(const asd_gated& p, Carve* c) {
+  const int e = type_bytes(p.type);
+  GatedPlan r;
+  r.x = operand(p.x, p.rows, p.cols, p.ld_x, e, c);
+  r.g = operand(p.w_gate, p.channels, p.cols, p.ld_w_gate, e, c);
+  r.u = operand(p.w_up, p.channels, p.cols, p.ld_w_up, e, c);
+  r.bytes = c->used;
+  return r;
+}
+static RowsProduct gated_product(const asd_gated& p, const GatedPlan& o) {
+  return RowsProduct{o.x.p, o.g.p, o.u.p, o.x.pitch, o.g.pitch, o.u.pitch, p.rows, p.channels, k_bytes((int64_t)p.cols * type_bytes(p.type)), p.rows_used};
+}
+
+template <class E, class T>
+static asd_status run_gated(const asd_gated& p, const GatedPlan& o, hipStream_t st) {
+  const bool wide = on16(p.out, p.ld_out, sizeof(T));
+  if constexpr (E::kBytes == 1) {
+    const Gated8Epi<T> e{static_cast<T*>(p.out), p.ld_out, p.x_scale, p.gate_scale, p.up_scale, p.channels, p.act, wide};
+    ASD_HIP(launch_product<E>(gated_product(p, o), e, st));
+  } else {
+    const GatedEpi<T> e{static_cast<T*>(p.out), p.ld_out, p.channels, p.act, wide};
+    ASD_HIP(launch_product<E>(gated_product(p, o), e, st));
+  }
+  return ASD_OK;
+}
+
+asd_status launch_gated(const asd_gated& p, hipStream_t st) {
+  Carve c{static_cast<uint8_t*>(p.workspace)};
+  const GatedPlan o = plan_gated(p, &c);
+  ASD_HIP(bring(o.x, st));
+  ASD_HIP(bring(o.g, st));
+  ASD_HIP(bring(o.u, st));
+  if (p.type == ASD_I8) return p.out_type == ASD_BF16 ? run_gated<ElemI8, __bf16>(p, o, st) : run_gated<ElemI8, _Float16>(p, o, st);
+  return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st) : run_gated<ElemF16, _Float16>(p, o, st);
+}
+
+// Gradient.  g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
+// over an index that is not the operands' rows' own (channels, rows), so their operands are transposed first, in passes that
+// cost a twentieth of the products at training sizes.
+struct GatedGradPlan {
+  GatedPlan in;
+  int Np;        // channels, padded to whole stages of k
+  int64_t Mp;    // rows, likewise
+  uint8_t *dgu, *dgu_t, *w_t, *x_t;
+  size_t bytes;
+};
+static GatedGradPlan plan_gated_grad(const asd_gated& p) {
+  Carve c{static_cast<uint8_t*>(p.workspace)};
+  GatedGradPlan r;
+  r.in = plan_gated(p, &c);
+  r.Np = (int)(ceil_div(p.channels, 64) * 64);
+  r.Mp = ceil_div(p.rows, 64) * 64;
+  r.dgu = c.take((size_t)2 * p.rows * 2 * r.Np);
+  r.w_t = p.dx ? c.take((size_t)2 * p.cols * 2 * r.Np) : nullptr;
+  r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * r.Mp) : nullptr;
+  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * r.Mp) : nullptr;
+  r.bytes = c.used;
+  return r;
+}
+
+static hipError_t transpose16(const void* src, int64_t ld, int rows, int cols, uint8_t* dst, int64_t dst_ld, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 64));
+  hipLaunchKernelGGL(transpose16_kernel, grid, dim3(256), 0, st, static_cast<const uint16_t*>(src), ld, rows, cols, on16(src, ld, 2) ? 1 : 0,
+                     reinterpret_cast<uint16_t*>(dst), dst_ld);
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void zero16_kernel(uint16_t* p, int64_t ld, int rows, int cols) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at < (int64_t)rows * cols) p[at / cols * ld + at % cols] = 0;
+}
+
+template <class E, class T>
+static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
+  const GatedGradPlan o = plan_gated_grad(p);
+  ASD_HIP(bring(o.in.x, st));
+  ASD_HIP(bring(o.in.g, st));
+  ASD_HIP(bring(o.in.u, st));
+  T* dgu = reinterpret_cast<T*>(o.dgu);
+  const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act};
+  ASD_HIP(launch_product<E>(gated_product(p, o.in), e, st));
+  if (p.dx) {
+    ASD_HIP(transpose16(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, 2 * o.Np, st));
+    ASD_HIP(transpose16(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, 2 * o.Np, st));
+    const RowsProduct g{o.dgu, o.w_t, nullptr, 4 * (int64_t)o.Np, 4 * (int64_t)o.Np, 0, p.rows, p.cols, 4 * (int64_t)o.Np, nullptr};
+    const SumEpi<T> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
+    ASD_HIP(launch_product<E>(g, s, st));
+  }
+  if (p.dw_gate) {
+    ASD_HIP(transpose16(o.dgu, 2 * o.Np, p.rows, 2 * o.Np, o.dgu_t, o.Mp, st));
+    ASD_HIP(transpose16(p.x, p.ld_x, p.rows, p.cols, o.x_t, o.Mp, st));
+    const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * o.Mp, 2 * o.Mp, 0, 2 * o.Np, p.cols, 2 * o.Mp, nullptr};
+    const SumEpi<T> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
+                      on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
+    ASD_HIP(launch_product<E>(g, s, st));
+  }
+  return ASD_OK;
+}
+
+// ---- checks --------------------------------------------------------------------------------------------------------------------
+constexpr int kMaxI8Cols = 131071;         // 2^14 times as many fits 31 bits
+constexpr int kMaxCols = 1 << 20;
+
+static asd_status check_sizes(int rows, int cols, int channels) {
+  if (rows < 0 || cols < 1 || channels < 1)
+    return fail(ASD_EINVAL, "rows must be >= 0, cols and channels >= 1 (got %d, %d, %d)", rows, cols, channels);
+  if (rows > (1 << 28) || channels > (1 << 28)) return fail(ASD_EUNSUPPORTED, "rows and channels up to 2^28 (got %d, %d)", rows, channels);
+  return ASD_OK;
+}
+static asd_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (need && (!ws || have < need || ((uintptr_t)ws & 15)))
+    return fail(ASD_EINVAL, "workspace: %zu bytes at a multiple of 16 are needed", need);
+  return ASD_OK;
+}
+
+static asd_status check_linear8(const asd_linear8* p) {
+  if (!p) return fail(ASD_EINVAL, "arguments are NULL");
+  ASD_TRY(check_sizes(p->rows, p->cols, p->channels));
+  if (p->cols > kMaxI8Cols) return fail(ASD_EUNSUPPORTED, "cols > %d: a sum may leave 32 bits (got %d)", kMaxI8Cols, p->cols);
+  if (!float_type(p->out_type)) return fail(ASD_EINVAL, "unknown out_type %d", p->out_type);
+  if (p->rows == 0) return ASD_OK;
+  if (!p->x || !p->x_scale || !p->w || !p->w_scale || !p->out) return fail(ASD_EINVAL, "a pointer is NULL");
+  const MatArg m[] = {{"out", p->out, p->rows, p->channels, p->ld_out, type_bytes(p->out_type), true},
+                      {"workspace", p->workspace, p->workspace_bytes ? 1 : 0, (int64_t)p->workspace_bytes, (int64_t)p->workspace_bytes, 1, true},
+                      {"x", p->x, p->rows, p->cols, p->ld_x, 1, false},
+                      {"w", p->w, p->channels, p->cols, p->ld_w, 1, false},
+                      {"x_scale", p->x_scale, 1, p->rows, p->rows, 4, false},
+                      {"w_scale", p->w_scale, 1, p->channels, p->channels, 4, false},
+                      {"bias", p->bias, 1, p->channels, p->channels, 4, false},
+                      {"rows_used", p->rows_used, 1, 1, 1, 4, false}};
+  ASD_TRY(check_mats(m, 8));
+  return check_workspace(p->workspace, p->workspace_bytes, plan_linear8(*p, nullptr).bytes);
+}
+
+static asd_status check_gated(const asd_gated* p, bool backward) {
+  if (!p) return fail(ASD_EINVAL, "arguments are NULL");
+  ASD_TRY(check_sizes(p->rows, p->cols, p->channels));
+  if (!half_type(p->type) && (backward || p->type != ASD_I8)) return fail(ASD_EINVAL, "type %d is not one of the unit's", p->type);
+  if (!half_type(p->type) && p->cols > kMaxI8Cols) return fail(ASD_EUNSUPPORTED, "cols > %d: a sum may leave 32 bits (got %d)", kMaxI8Cols, p->cols);
+  if (p->cols > kMaxCols) return fail(ASD_EUNSUPPORTED, "cols > %d (got %d)", kMaxCols, p->cols);
+  if (p->act != ASD_ACT_SILU && p->act != ASD_ACT_GELU) return fail(ASD_EINVAL, "unknown activation %d", p->act);
+  if (backward && (p->rows > kMaxCols || p->channels > kMaxCols)) return fail(ASD_EUNSUPPORTED, "gradients: rows and channels up to %d", kMaxCols);
+  if (backward && p->rows_used) return fail(ASD_EINVAL, "gradients take no rows_used");
+  if (backward && (p->dw_gate != nullptr) != (p->dw_up != nullptr)) return fail(ASD_EINVAL, "dw_gate and dw_up go together");
+  if (!backward && (p->type == ASD_I8 ? !half_type(p->out_type) : p->out_type != p->type))
+    return fail(ASD_EINVAL, "out_type %d does not go with type %d", p->out_type, p->type);
+  if (p->rows == 0 && !backward) return ASD_OK;
+  if (p->rows > 0) {
+    if (!p->x || !p->w_gate || !p->w_up) return fail(ASD_EINVAL, "a pointer is NULL");
+    if (!backward && !p->out) return fail(ASD_EINVAL, "out is NULL");
+    if (backward && !p->dh) return fail(ASD_EINVAL, "dh is NULL");
+    if (p->type == ASD_I8 && (!p->x_scale || !p->gate_scale || !p->up_scale)) return fail(ASD_EINVAL, "8-bit operands need their scales");
+  }
+  const int e = type_bytes(p->type), oe = backward ? e : type_bytes(p->out_type);
+  const bool i8 = p->type == ASD_I8;
+  const MatArg m[] = {{"out", backward ? nullptr : p->out, p->rows, p->channels, p->ld_out, oe, true},
+                      {"dx", backward ? p->dx : nullptr, p->rows, p->cols, p->ld_dx, e, true},
+                      {"dw_gate", backward ? p->dw_gate : nullptr, p->channels, p->cols, p->ld_dw_gate, e, true},
+                      {"dw_up", backward ? p->dw_up : nullptr, p->channels, p->cols, p->ld_dw_up, e, true},
+                      {"workspace", p->workspace, p->workspace_bytes ? 1 : 0, (int64_t)p->workspace_bytes, (int64_t)p->workspace_bytes, 1, true},
+                      {"x", p->x, p->rows, p->cols, p->ld_x, e, false},
+                      {"w_gate", p->w_gate, p->channels, p->cols, p->ld_w_gate, e, false},
+                      {"w_up", p->w_up, p->channels, p->cols, p->ld_w_up, e, false},
+                      {"dh", backward ? p->dh : nullptr, p->rows, p->channels, p->ld_dh, e, false},
+                      {"x_scale", i8 ? p->x_scale : nullptr, 1, p->rows, p->rows, 4, false},
+                      {"gate_scale", i8 ? p->gate_scale : nullptr, 1, p->channels, p->channels, 4, false},
+                      {"up_scale", i8 ? p->up_scale : nullptr, 1, p->channels, p->channels, 4, false},
+                      {"rows_used", p->rows_used, 1, 1, 1, 4, false}};
+  ASD_TRY(check_mats(m, 13));
+  if (p->rows == 0) return ASD_OK;
+  asd_gated q = *p;
+  q.workspace = nullptr;
+  Carve c{nullptr};
+  return check_workspace(p->workspace, p->workspace_bytes, backward ? plan_gated_grad(q).bytes : plan_gated(q, &c).bytes);
+}
+
+}  // namespace asd
+
+using namespace asd;
+
+extern "C" {
+
+size_t asd_linear_i8_workspace(const asd_linear8* p) {
+  return !p || p->rows < 1 || p->cols < 1 || p->channels < 1 ? 0 : plan_linear8(*p, nullptr).bytes;
+}
+
+asd_status asd_linear_i8(const asd_linear8* p, void* stream) {
+  ASD_TRY(check_linear8(p));
+  return p->rows ? launch_linear8(*p, (hipStream_t)stream) : ASD_OK;
+}
+
+size_t asd_gated_ff_workspace(const asd_gated* p) {
+  if (!p || p->rows < 1 || p->cols < 1 || p->channels < 1) return 0;
+  Carve c{nullptr};
+  return plan_gated(*p, &c).bytes;
+}
+
+asd_status asd_gated_ff(const asd_gated* p, void* stream) {
+  ASD_TRY(check_gated(p, false));
+  return p->rows ? launch_gated(*p, (hipStream_t)stream) : ASD_OK;
+}
+
+size_t asd_gated_ff_backward_workspace(const asd_gated* p) {
+  if (!p || p->rows < 1 || p->cols < 1 || p->channels < 1) return 0;
+  asd_gated q = *p;
+  q.workspace = nullptr;
+  return plan_gated_grad(q).bytes;
+}
+
+asd_status asd_gated_ff_backward(const asd_gated* p, void* stream) {
+  ASD_TRY(check_gated(p, true));
+  const hipStream_t st = (hipStream_t)stream;
+  if (p->rows == 0) {
+    const int64_t n = (int64_t)p->channels * p->cols;
+    if (p->dw_gate) {
+      hipLaunchKernelGGL(zero16_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, static_cast<uint16_t*>(p->dw_gate), p->ld_dw_gate, p->channels, p->cols);
+      hipLaunchKernelGGL(zero16_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, static_cast<uint16_t*>(p->dw_up), p->ld_dw_up, p->channels, p->cols);
+      ASD_HIP(hipGetLastError());
+    }
+    return ASD_OK;
+  }
+  return p->type == ASD_BF16 ? run_gated_grad<ElemBf16, __bf16>(*p, st) : run_gated_grad<ElemF16, _Float16>(*p, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,429 @@
+// Root-mean-square norm of rows, with a residual added on the way in and 8-bit rows with scales on the way out; the row
+// quantiser on its own; and the norm's gradient.
+//
+//   r = x + residual,  rstd = (mean r^2 + eps)^(-1/2),  y = r rstd gain
+//   8 bits: v = r gain, q = nearest integer to 127 v / max |v|, scale = max |v| rstd / 127
+// rstd cancels from q: the integers depend on v alone, and a tie is a tie in exact arithmetic (v = max |v| / 2 is 63.5 steps, a
+// common case with 16-bit inputs).  So the squares' sum, v and the quotient are kept in 64 bits; the quotient, a multiplication
+// by the reciprocal with one step of correction (the remainder, exact in a fused multiply-add, times the reciprocal), is the
+// correctly rounded one, exact where it has to be.  The kernels are bound by memory; the 64-bit arithmetic, some ten
+// instructions a number at half the fp32 rate, runs under the loads.
+//
+// One pass: a row lies in the registers of a wavefront (up to 2048 numbers), a workgroup of four, or of sixteen; each
+// thread holds runs of eight, loaded 16 bytes at a time, or single numbers a stride apart where rows start at no multiple of
+// 16 bytes.
+#include <math.h>
+
+#include "ops.h"
+
+namespace asd {
+
+constexpr int kRun = 8;   // numbers a thread loads at once
+
+// Numbers a thread holds of a row: its c-th run of eight, or (wide false) eight single ones, `threads` apart.
+template <class T>
+__device__ __forceinline__ void load_run(const T* row, int cols, int threads, int t, bool wide, int c, float* v) {
+  const int first = (c * threads + t) * kRun;
+  if (wide && first + kRun <= cols) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 a = *reinterpret_cast<const float4*>(row + first), b = *reinterpret_cast<const float4*>(row + first + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      T h[kRun];
+      *reinterpret_cast<uint4*>(h) = *reinterpret_cast<const uint4*>(row + first);
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) v[k] = (float)h[k];
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kRun; ++k) {
+    const int i = wide ? first + k : (c * kRun + k) * threads + t;
+    v[k] = i < cols ? (float)row[i] : 0.f;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void store_run(T* row, int cols, int threads, int t, bool wide, int c, const T* v) {
+  const int first = (c * threads + t) * kRun;
+  if (wide && first + kRun <= cols) {
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<uint4*>(row + first) = *reinterpret_cast<const uint4*>(v);
+      *reinterpret_cast<uint4*>(row + first + 4) = *reinterpret_cast<const uint4*>(v + 4);
+    } else if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4*>(row + first) = *reinterpret_cast<const uint4*>(v);
+    } else {
+      *reinterpret_cast<uint2*>(row + first) = *reinterpret_cast<const uint2*>(v);
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kRun; ++k) {
+    const int i = wide ? first + k : (c * kRun + k) * threads + t;
+    if (i < cols) row[i] = v[k];
+  }
+}
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ double wave_max64(double v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = fmax(v, __shfl_xor(v, d));
+  return v;
+}
+
+// Sums (and the largest of `top`) over the THREADS threads of a row, in every one of them.  The parts of a workgroup's wavefronts
+// are added in their order.
+template <int THREADS>
+__device__ __forceinline__ void row_total(double& a, double& b, double& top, double (*lds)[3]) {
+  a = wave_sum64(a);
+  b = wave_sum64(b);
+  top = wave_max64(top);
+  if constexpr (THREADS > 64) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();   // (the last row's parts have been read)
+    if ((threadIdx.x & 63) == 0) {
+      lds[wave][0] = a;
+      lds[wave][1] = b;
+      lds[wave][2] = top;
+    }
+    __syncthreads();
+    a = b = top = 0.0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      a += lds[w][0];
+      b += lds[w][1];
+      top = fmax(top, lds[w][2]);
+    }
+  }
+}
+
+// x, residual, sum and gain of type T; out of type O (int8_t: with scales).  THREADS threads a row, RUNS runs a thread.
+template <class T, class O, int THREADS, int RUNS, bool NORM>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel(asd_norm p, int wide) {
+  constexpr bool I8 = sizeof(O) == 1;
+  constexpr int PER_WG = THREADS < 256 ? 256 / THREADS : 1;
+  __shared__ double lds[THREADS / 64][3];
+  const int rows = p.rows_used ? min(max(*p.rows_used, 0), p.rows) : p.rows;
+  const int t = threadIdx.x % THREADS;
+  const int row = (int)blockIdx.x * PER_WG + (PER_WG > 1 ? (int)threadIdx.x / THREADS : 0);
+  if (row >= rows) return;   // (whole workgroups, or wavefronts that wait for nobody)
+  const T* x = static_cast<const T*>(p.x) + row * p.ld_x;
+  const T* res = NORM && p.residual ? static_cast<const T*>(p.residual) + row * p.ld_residual : nullptr;
+  const T* gain = NORM ? static_cast<const T*>(p.gain) : nullptr;
+  float r[RUNS][kRun];
+#pragma unroll
+  for (int c = 0; c < RUNS; ++c) load_run(x, p.cols, THREADS, t, wide & 1, c, r[c]);
+  if (res) {
+    float q[RUNS][kRun];
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) load_run(res, p.cols, THREADS, t, wide & 1, c, q[c]);
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c)
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) r[c][k] += q[c][k];
+  }
+  if (NORM && p.sum) {
+    T* sum = static_cast<T*>(p.sum) + row * p.ld_sum;
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      T v[kRun];
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) v[k] = (T)r[c][k];
+      store_run(sum, p.cols, THREADS, t, wide & 1, c, v);
+    }
+  }
+  float g[RUNS][kRun];
+#pragma unroll
+  for (int c = 0; c < RUNS; ++c) {
+    if (gain) load_run(gain, p.cols, THREADS, t, wide & 1, c, g[c]);
+    else
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) g[c][k] = 1.f;
+  }
+  // odd: NaN as soon as one of the row's v is not a number below infinity
+  double squares = 0.0, odd = 0.0, top = 0.0;
+#pragma unroll
+  for (int c = 0; c < RUNS; ++c)
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      const double d = (double)r[c][k];
+      if constexpr (NORM) squares = fma(d, d, squares);
+      if constexpr (I8) {
+        const double v = NORM ? d * (double)g[c][k] : d;
+        odd = fma(v, 0.0, odd);
+        top = fmax(top, fabs(v));
+      }
+    }
+  row_total<THREADS>(squares, odd, top, lds);
+  const double rstd = NORM ? 1.0 / sqrt(squares / (double)p.cols + p.eps) : 1.0;
+  O* out = static_cast<O*>(p.out) + row * p.ld_out;
+  if constexpr (I8) {
+    const bool good = odd == 0.0 && (!NORM || squares < INFINITY);
+    const double inv = 1.0 / top;
+    if (t == 0) p.scale[row] = !good ? __uint_as_float(0x7fc00000u) : top > 0.0 ? (float)(top * rstd / 127.0) : 0.f;
+    const bool some = good && top > 0.0;
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      int8_t q[kRun];
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) {
+        const double d = (double)r[c][k], a = 127.0 * (NORM ? d * (double)g[c][k] : d);
+        const double q0 = a * inv, q1 = fma(fma(-q0, top, a), inv, q0);
+        q[k] = some ? (int8_t)(int)rint(q1) : (int8_t)0;
+      }
+      store_run(out, p.cols, THREADS, t, wide & 2, c, q);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      O v[kRun];
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) v[k] = (O)((float)((double)r[c][k] * rstd) * g[c][k]);   // (rstd alone may leave fp32)
+      store_run(out, p.cols, THREADS, t, wide & 2, c, v);
+    }
+  }
+}
+
+// Gradient.  A workgroup takes every gridDim.x-th row, and adds dy n up by column as it goes; the columns' parts, one row of them
+// for each workgroup, are added in their order by the second kernel.
+template <class T, int THREADS, int RUNS>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_grad_kernel(asd_norm_grad p, int wide, float* parts) {
+  constexpr int PER_WG = THREADS < 256 ? 256 / THREADS : 1;
+  __shared__ double lds[THREADS / 64][3];
+  const int t = threadIdx.x % THREADS, lane_row = PER_WG > 1 ? (int)threadIdx.x / THREADS : 0;
+  const int part = (int)blockIdx.x * PER_WG + lane_row, n_parts = (int)gridDim.x * PER_WG;
+  float g[RUNS][kRun], dg[RUNS][kRun];
+#pragma unroll
+  for (int c = 0; c < RUNS; ++c) {
+    if (p.gain) load_run(static_cast<const T*>(p.gain), p.cols, THREADS, t, wide & 1, c, g[c]);
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      if (!p.gain) g[c][k] = 1.f;
+      dg[c][k] = 0.f;
+    }
+  }
+  for (int row = part; row < p.rows; row += n_parts) {
+    float r[RUNS][kRun], dy[RUNS][kRun];
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      load_run(static_cast<const T*>(p.sum) + row * p.ld_sum, p.cols, THREADS, t, wide & 1, c, r[c]);
+      load_run(static_cast<const T*>(p.dy) + row * p.ld_dy, p.cols, THREADS, t, wide & 1, c, dy[c]);
+    }
+    double squares = 0.0, along = 0.0, none = 0.0;
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c)
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) {
+        const double d = (double)r[c][k];
+        squares = fma(d, d, squares);
+        along = fma((double)(g[c][k] * dy[c][k]), d, along);
+      }
+    row_total<THREADS>(squares, along, none, lds);
+    const double rs = 1.0 / sqrt(squares / (double)p.cols + p.eps);
+    const float rstd = (float)rs, mean = (float)(along * rs / (double)p.cols);
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c)
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) r[c][k] = (float)((double)r[c][k] * rs);   // n from here on
+    if (p.dx) {
+      const T* ds = p.dsum ? static_cast<const T*>(p.dsum) + row * p.ld_dsum : nullptr;
+#pragma unroll
+      for (int c = 0; c < RUNS; ++c) {
+        float q[kRun];
+        T v[kRun];
+        if (ds) load_run(ds, p.cols, THREADS, t, wide & 1, c, q);
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+          const float d = rstd * (g[c][k] * dy[c][k] - r[c][k] * mean);
+          v[k] = (T)(ds ? d + q[k] : d);
+        }
+        store_run(static_cast<T*>(p.dx) + row * p.ld_dx, p.cols, THREADS, t, wide & 1, c, v);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c)
+#pragma unroll
+      for (int k = 0; k < kRun; ++k) dg[c][k] = fmaf(dy[c][k], r[c][k], dg[c][k]);
+  }
+  if (parts)
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) store_run(parts + (int64_t)part * p.cols, p.cols, THREADS, t, (wide & 1) && (p.cols & 3) == 0, c, dg[c]);
+}
+
+// dgain: 64 columns a workgroup, its four wavefronts take every fourth part, in order.
+template <class T>
+__global__ __launch_bounds__(256) void norm_gain_grad_kernel(int cols, int n_parts, const float* __restrict__ parts, T* __restrict__ dgain) {
+  __shared__ float lds[4][64];
+  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+  float s = 0.f;
+  if (col < cols)
+#pragma unroll 8
+    for (int i = wave; i < n_parts; i += 4) s += parts[(int64_t)i * cols + col];
+  lds[wave][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (wave == 0 && col < cols) dgain[col] = (T)((lds[0][threadIdx.x] + lds[1][threadIdx.x]) + (lds[2][threadIdx.x] + lds[3][threadIdx.x]));
+}
+
+// f(threads, runs) as constants for rows of `cols`: the fewest threads that hold one in four runs each (up to 2048 numbers a
+// wavefront, 8192 four, 32768 sixteen), then eight runs.
+template <class F>
+static asd_status by_width(int cols, F f) {
+  typedef std::integral_constant<int, 64> W1;
+  typedef std::integral_constant<int, 256> W4;
+  typedef std::integral_constant<int, 1024> W16;
+  const auto runs = [&](int threads) { return (int)ceil_div(cols, threads * kRun); };
+  if (runs(64) <= 1) return f(W1(), std::integral_constant<int, 1>());
+  if (runs(64) <= 2) return f(W1(), std::integral_constant<int, 2>());
+  if (runs(256) <= 1) return f(W4(), std::integral_constant<int, 1>());
+  if (runs(256) <= 2) return f(W4(), std::integral_constant<int, 2>());
+  if (runs(256) <= 4) return f(W4(), std::integral_constant<int, 4>());
+  if (runs(1024) <= 2) return f(W16(), std::integral_constant<int, 2>());
+  if (runs(1024) <= 4) return f(W16(), std::integral_constant<int, 4>());
+  return f(W16(), std::integral_constant<int, 8>());
+}
+
+constexpr int kMaxNormCols = 65536;
+
+template <class T, class O, bool NORM>
+static asd_status run_norm(const asd_norm& p, hipStream_t st) {
+  int wide = on16(p.x, p.ld_x, sizeof(T)) ? 1 : 0;
+  if (NORM) {
+    if ((p.residual && !on16(p.residual, p.ld_residual, sizeof(T))) || (p.sum && !on16(p.sum, p.ld_sum, sizeof(T))) ||
+        (p.gain && ((uintptr_t)p.gain & 15)))
+      wide = 0;
+  }
+  // (runs of eight int8 are eight bytes; a thread's numbers are the same ones on the way in and out)
+  const bool out_wide = sizeof(O) == 1 ? ((uintptr_t)p.out & 7) == 0 && (p.ld_out & 7) == 0 : on16(p.out, p.ld_out, sizeof(O));
+  wide = wide && out_wide ? 3 : 0;
+  return by_width(p.cols, [&](auto threads, auto runs) -> asd_status {
+    constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
+    hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM>), dim3((unsigned)ceil_div(p.rows, PER)), dim3(TH * PER), 0, st, p, wide);
+    ASD_HIP(hipGetLastError());
+    return ASD_OK;
+  });
+}
+
+template <class T>
+static asd_status run_norm_to(const asd_norm& p, hipStream_t st) {
+  switch (p.out_type) {
+    case ASD_F32: return run_norm<T, float, true>(p, st);
+    case ASD_BF16: return run_norm<T, __bf16, true>(p, st);
+    case ASD_F16: return run_norm<T, _Float16, true>(p, st);
+    default: return run_norm<T, int8_t, true>(p, st);
+  }
+}
+
+asd_status launch_rms_norm(const asd_norm& p, hipStream_t st) {
+  return p.type == ASD_F32 ? run_norm_to<float>(p, st) : p.type == ASD_BF16 ? run_norm_to<__bf16>(p, st) : run_norm_to<_Float16>(p, st);
+}
+
+asd_status launch_quantize_rows(const asd_norm& p, hipStream_t st) {
+  return p.type == ASD_F32    ? run_norm<float, int8_t, false>(p, st)
+         : p.type == ASD_BF16 ? run_norm<__bf16, int8_t, false>(p, st)
+                              : run_norm<_Float16, int8_t, false>(p, st);
+}
+
+static asd_status check_norm_sizes(int rows, int cols, int type) {
+  if (rows < 0 || cols < 1) return fail(ASD_EINVAL, "rows must be >= 0 and cols >= 1 (got %d, %d)", rows, cols);
+  if (!float_type(type)) return fail(ASD_EINVAL, "type %d is not a number type", type);
+  if (cols > kMaxNormCols) return fail(ASD_EUNSUPPORTED, "cols > %d (got %d)", kMaxNormCols, cols);
+  return ASD_OK;
+}
+
+static asd_status check_norm(const asd_norm* p, bool norm) {
+  if (!p) return fail(ASD_EINVAL, "arguments are NULL");
+  ASD_TRY(check_norm_sizes(p->rows, p->cols, p->type));
+  const int out_type = norm ? p->out_type : ASD_I8;
+  if (!float_type(out_type) && out_type != ASD_I8) return fail(ASD_EINVAL, "unknown out_type %d", out_type);
+  if (norm && !(p->eps >= 0.0 && p->eps < INFINITY)) return fail(ASD_EINVAL, "eps must be finite and >= 0");
+  if (p->rows == 0) return ASD_OK;
+  if (!p->x || !p->out) return fail(ASD_EINVAL, "%s is NULL", !p->x ? "x" : "out");
+  if (out_type == ASD_I8 && !p->scale) return fail(ASD_EINVAL, "8-bit rows need scale");
+  const int e = type_bytes(p->type);
+  const MatArg m[] = {{"sum", norm ? p->sum : nullptr, p->rows, p->cols, p->ld_sum, e, true},
+                      {"out", p->out, p->rows, p->cols, p->ld_out, type_bytes(out_type), true},
+                      {"scale", out_type == ASD_I8 ? p->scale : nullptr, 1, p->rows, p->rows, 4, true},
+                      {"x", p->x, p->rows, p->cols, p->ld_x, e, false},
+                      {"residual", norm ? p->residual : nullptr, p->rows, p->cols, p->ld_residual, e, false},
+                      {"gain", norm ? p->gain : nullptr, 1, p->cols, p->cols, e, false},
+                      {"rows_used", p->rows_used, 1, 1, 1, 4, false}};
+  return check_mats(m, 7, [](int i, int j) { return i == 0 && (j == 3 || j == 4); });
+}
+
+// Parts of dgain: enough workgroups to fill the chip (four of 256 threads a CU), no more than eight rows leave worth a part.
+static int norm_grad_wgs(int rows, int cols) {
+  const int per_wg = cols <= 2 * 64 * kRun ? 4 : 1;   // rows a workgroup takes at a time (by_width)
+  return (int)std::max<int64_t>(1, std::min<int64_t>(1024, ceil_div(rows, 8 * per_wg)));
+}
+static int norm_grad_parts(int rows, int cols) { return norm_grad_wgs(rows, cols) * (cols <= 2 * 64 * kRun ? 4 : 1); }
+
+template <class T>
+static asd_status run_norm_grad(const asd_norm_grad& p, hipStream_t st) {
+  int wide = on16(p.dy, p.ld_dy, sizeof(T)) && on16(p.sum, p.ld_sum, sizeof(T)) && (!p.gain || ((uintptr_t)p.gain & 15) == 0) &&
+             (!p.dsum || on16(p.dsum, p.ld_dsum, sizeof(T))) && (!p.dx || on16(p.dx, p.ld_dx, sizeof(T)));
+  float* parts = p.dgain ? static_cast<float*>(p.workspace) : nullptr;
+  if (p.rows > 0) {
+    ASD_TRY(by_width(p.cols, [&](auto threads, auto runs) -> asd_status {
+      constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
+      hipLaunchKernelGGL((rms_norm_grad_kernel<T, TH, R>), dim3((unsigned)norm_grad_wgs(p.rows, p.cols)), dim3(TH * PER), 0, st, p, wide,
+                         parts);
+      ASD_HIP(hipGetLastError());
+      return ASD_OK;
+    }));
+  }
+  if (p.dgain) {
+    hipLaunchKernelGGL((norm_gain_grad_kernel<T>), dim3((unsigned)ceil_div(p.cols, 64)), dim3(256), 0, st, p.cols,
+                       p.rows > 0 ? norm_grad_parts(p.rows, p.cols) : 0, parts, static_cast<T*>(p.dgain));
+    ASD_HIP(hipGetLastError());
+  }
+  return ASD_OK;
+}
+
+}  // namespace asd
+
+using namespace asd;
+
+extern "C" {
+
+asd_status asd_rms_norm(const asd_norm* p, void* stream) {
+  ASD_TRY(check_norm(p, true));
+  return p->rows ? launch_rms_norm(*p, (hipStream_t)stream) : ASD_OK;
+}
+
+asd_status asd_quantize_rows(const asd_norm* p, void* stream) {
+  ASD_TRY(check_norm(p, false));
+  return p->rows ? launch_quantize_rows(*p, (hipStream_t)stream) : ASD_OK;
+}
+
+size_t asd_rms_norm_backward_workspace(const asd_norm_grad* p) {
+  if (!p || !p->dgain || p->rows < 1 || p->cols < 1) return 0;
+  return sizeof(float) * (size_t)norm_grad_parts(p->rows, p->cols) * (size_t)p->cols;
+}
+
+asd_status asd_rms_norm_backward(const asd_norm_grad* p, void* stream) {
+  if (!p) return fail(ASD_EINVAL, "arguments are NULL");
+  ASD_TRY(check_norm_sizes(p->rows, p->cols, p->type));
+  if (!(p->eps >= 0.0 && p->eps < INFINITY)) return fail(ASD_EINVAL, "eps must be finite and >= 0");
+  if (p->rows > 0 && (!p->dy || !p->sum)) return fail(ASD_EINVAL, "%s is NULL", !p->dy ? "dy" : "sum");
+  const int e = type_bytes(p->type);
+  const MatArg m[] = {{"dx", p->dx, p->rows, p->cols, p->ld_dx, e, true},
+                      {"dgain", p->dgain, 1, p->cols, p->cols, e, true},
+                      {"workspace", p->workspace, p->workspace && p->workspace_bytes ? 1 : 0, (int64_t)p->workspace_bytes, (int64_t)p->workspace_bytes, 1, true},
+                      {"dy", p->dy, p->rows, p->cols, p->ld_dy, e, false},
+                      {"sum", p->sum, p->rows, p->cols, p->ld_sum, e, false},
+                      {"gain", p->gain, 1, p->cols, p->cols, e, false},
+                      {"dsum", p->dsum, p->rows, p->cols, p->ld_dsum, e, false}};
+  ASD_TRY(check_mats(m, 7, [](int i, int j) { return i == 0 && (j == 3 || j == 6); }));
+  const size_t need = asd_rms_norm_backward_workspace(p);
+  if (need && (!p->workspace || p->workspace_bytes < need || ((uintptr_t)p->workspace & 15)))
+    return fail(ASD_EINVAL, "workspace: %zu bytes at a multiple of 16 are needed", need);
+  const hipStream_t st = (hipStream_t)stream;
+  return p->type == ASD_F32 ? run_norm_grad<float>(*p, st) : p->type == ASD_BF16 ? run_norm_grad<__bf16>(*p, st) : run_norm_grad<_Float16>(*p, st);
+}
+
+}  // extern "C"
