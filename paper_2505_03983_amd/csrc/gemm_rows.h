@@ -120,6 +120,64 @@ __device__ __forceinline__ bool rows_tile(int tiles_m, int tiles_n, int* tm, int
   return true;
 }
 
+// Epilogue.  acc[j][i]: blocks of B x B results (B = 32 or 16 by the matrix instruction), channels by rows; a lane holds, of its
+// row of a block, four channels at 4 (lane / B), and with B = 32 those 8, 16 and 24 further on.  The results go through LDS, in
+// the output's type, 64 columns a wavefront or 32 where two factors become one, so that rows leave in whole runs; LDS slots of 16
+// bytes are permuted by the row for the banks.
+template <class E, class Cfg, class Epi, class Acc, int NB, int MB>
+__device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB], uint8_t* lds, int m0, int n0, int M) {
+  constexpr bool GATED = Epi::kGated;
+  constexpr int NW = Cfg::NW, B = Cfg::WN / NB;
+  constexpr int RUNS = B == 32 ? 4 : 1;                     // a lane's runs of four channels in a block
+  lds_handover();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / Cfg::WGN, wn = wave % Cfg::WGN;
+  const int lrow = lane % B, part = lane / B;
+  typedef typename Epi::Out Out;
+  constexpr int COLS = Cfg::WN / (GATED ? 2 : 1), OB = (int)sizeof(Out);
+  constexpr int ROWB = COLS * OB, SL = ROWB / 16;           // bytes and slots of a row
+  static_assert(NW * B * ROWB <= Cfg::PIPE_BYTES, "parked results");
+  static_assert(SL >= 2 && SL <= 64 && (SL & (SL - 1)) == 0, "slots of a parked row");
+  constexpr int FACTOR = GATED ? 32 / B : 0;                // blocks from a gate's to the matching up's
+  uint8_t* park = lds + wave * (B * ROWB);
+  const int col0 = n0 + wn * COLS;                          // channel of the wavefront's first column
+  for (int out = 0; out < Epi::kOutputs; ++out) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const int mrow = m0 + wm * Cfg::WM + i * B;
+      if (mrow >= M) break;
+      const int m = min(mrow + lrow, M - 1);
+      const auto rc = epi.row(m);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if (GATED && (j * B / 32) % 2) continue;
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) {
+          const int c = (GATED ? j * B / 64 * 32 + j * B % 32 : j * B) + (B == 32 ? 8 * q : 0) + 4 * part;
+          typename E::Sum a[4], b[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            a[r] = acc[j][i][4 * q + r];
+            b[r] = acc[j + FACTOR][i][4 * q + r];
+          }
+          Out v[4];
+          epi.values(out, rc, m, col0 + c, a, b, v);
+          const int byte = c * OB, sl = (byte >> 4) ^ (lrow & (SL - 1));
+          if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + lrow * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v);
+          else *reinterpret_cast<uint4*>(park + lrow * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v);
+        }
+      }
+      // (the region is this wavefront's own, whose LDS operations complete in order)
+      constexpr int RPI = 64 / SL < B ? 64 / SL : B;        // rows a pass of the wavefront covers
+#pragma unroll
+      for (int r0 = 0; r0 < B; r0 += RPI) {
+        const int r = r0 + lane / SL, sl = lane % SL;
+        const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
+        if (lane < RPI * SL && mrow + r < M) epi.store(out, mrow + r, col0 + sl * (16 / OB), v);
+      }
+    }
+  }
+}
+
 template <class E, class Cfg, class Epi>
 __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
   constexpr bool GATED = Epi::kGated;
@@ -269,52 +327,173 @@ __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, 
   for (; kt + STAGES - 1 < nk; ++kt) step(kt, std::true_type());
   for (; kt < nk; ++kt) step(kt, std::false_type());
 
-  // ---- epilogue.  A lane holds, for each of its MI rows, four channels at 8 q + 4 half of each group of 32.  The results go
-  // through LDS (the stages are free) in the output's type, 64 columns a wavefront or 32 where two factors become one, so
-  // that rows leave in whole runs; LDS slots of 16 bytes are permuted by the row for the banks.
-  lds_handover();
-  typedef typename Epi::Out Out;
-  constexpr int COLS = Cfg::WN / (GATED ? 2 : 1), OB = (int)sizeof(Out);
-  constexpr int ROWB = COLS * OB, SL = ROWB / 16;           // bytes and slots of a row
-  constexpr int ROWS = 32;                                  // rows parked at a time: one row group
-  static_assert(NW * ROWS * ROWB <= Cfg::PIPE_BYTES, "parked results");
-  static_assert(SL >= 2 && SL <= 64 && (SL & (SL - 1)) == 0, "slots of a parked row");
-  uint8_t* park = rows_lds + wave * (ROWS * ROWB);
-  const int col0 = n0 + wn * COLS;                          // channel of the wavefront's first column
-  for (int out = 0; out < Epi::kOutputs; ++out) {
+  rows_epilogue<E, Cfg>(epi, acc, rows_lds, m0, n0, M);
+}
+
+// ---- the large tile ----------------------------------------------------------------------------------------------------
+// 256 x 256 by eight wavefronts of 128 x 64, 128 bytes of k per stage, two stages (128 KB).  What bounds it is how fast a CU
+// pulls its operands: alone, the loads of 4096 such tiles run at 13.6 TB/s in rows of 64 bytes and at 19.0 in rows of 128, the
+// matrix cores ask for 14 at 1.9 GHz, and with all of a stage's loads waited for at its end (the pipeline above) 11.9 arrive.
+// So a stage is handed over in halves: the x rows a wavefront multiplies first (X0, half of its rows) with the channels it
+// multiplies first (W0), and the rest (X1, W1).  A stage takes two steps of 16 matrix instructions a wavefront,
+//   A: X0 W0, X0 W1     reads W1, X1 of this stage       fetches X0, W0 of the stage after the next
+//   B: X1 W0, X1 W1     reads X0, W0 of the next stage   fetches W1, X1 of the stage after the next
+// each half being refilled right after the step that has read it into registers: three steps of loads (96 KB) are always in
+// flight, and every step's operands are in registers when it starts.  One barrier a step.
+//
+// 16 x 16 instructions: of the same rate as the 32 x 32 ones of the other tiles, they read and write their sums half as often per
+// product, and this kernel is where the chip's power is the limit (1.5 GHz on random operands, 2.4 on zeros): 8192 x 32768 x 4096
+// in bf16 1703 us for 1800, and 1885 with the pipeline above.  (A workgroup that takes one tile after the other, the next one's
+// first stages under the results of the last, was no faster: 7.57 ms for 7.42 of a training step.)
+typedef RowsCfg<256, 256, 2, 4, 128, 2> Rows256;
+
+template <class E, class Epi>
+__global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
+  typedef Rows256 Cfg;
+  constexpr bool GATED = Epi::kGated;
+  constexpr int BM = 256, BKB = 128;
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
+
+  int tm, tn;
+  if (!rows_tile(tiles_m, tiles_n, &tm, &tn)) return;
+  const int M = p.rows_used ? min(max(*p.rows_used, 0), p.M) : p.M;
+  const int m0 = tm * BM, n0 = tn * (GATED ? 128 : 256);
+  if (m0 >= M) return;
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 2, wn = wave & 3, l16 = lane & 15, quarter = lane >> 4;
+
+  // A wavefront's loads of a half: 8 rows each, of x rows h * 64 + q * 128 + 8 wave .. (q = 0, 1), and of channel rows
+  // h * 32 + 64 (2 q + wave / 4) + 8 (wave % 4) ..  Slots of a row's eight chunks are permuted as above.
+  const __amdgpu_buffer_rsrc_t xr = rows_rsrc(p.x + (int64_t)m0 * p.x_pitch);
+  const __amdgpu_buffer_rsrc_t w0r = rows_rsrc(p.w0 + (int64_t)n0 * p.w_pitch0);
+  const __amdgpu_buffer_rsrc_t w1r = rows_rsrc(GATED ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0);
+  const int sub = lane >> 3, slot = lane & 7;
+  uint32_t x_off[2][2], w_off[2][2];
+  int x_blk[2][2], w_blk[2][2];                       // LDS, in kilobytes
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int mrow = m0 + wm * Cfg::WM + i * 32;
-      if (mrow >= M) break;
-      const int m = min(mrow + l32, M - 1);
-      const auto rc = epi.row(m);
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int j = 0; j < NJ; j += GATED ? 2 : 1)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int c = (GATED ? j / 2 : j) * 32 + 8 * q + 4 * half;
-          typename E::Sum a[4], b[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            a[r] = acc[j][i][4 * q + r];
-            b[r] = acc[GATED ? j + 1 : j][i][4 * q + r];
-          }
-          Out v[4];
-          epi.values(out, rc, m, col0 + c, a, b, v);
-          const int byte = c * OB, sl = (byte >> 4) ^ (l32 & (SL - 1));
-          if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + l32 * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v);
-          else *reinterpret_cast<uint4*>(park + l32 * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v);
-        }
-      // (the region is this wavefront's own, whose LDS operations complete in order)
-      constexpr int RPI = 64 / SL;                          // rows a pass of the wavefront covers
-#pragma unroll
-      for (int r0 = 0; r0 < ROWS; r0 += RPI) {
-        const int r = r0 + lane / SL, sl = lane % SL;
-        const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
-        if (mrow + r < M) epi.store(out, mrow + r, col0 + sl * (16 / OB), v);
-      }
+    for (int q = 0; q < 2; ++q) {
+      x_blk[h][q] = h * 8 + q * 16 + wave;
+      w_blk[h][q] = BM / 8 + h * 4 + 8 * (2 * q + (wave >> 2)) + (wave & 3);
+      const int xrow = x_blk[h][q] * 8 + sub, wrow = (w_blk[h][q] - BM / 8) * 8 + sub;
+      const int chunk = (slot ^ ((xrow >> 1) & 7)) * 16, wchunk = (slot ^ ((wrow >> 1) & 7)) * 16;
+      x_off[h][q] = (uint32_t)((int64_t)min(xrow, M - 1 - m0) * p.x_pitch) + chunk;
+      const int ch = GATED ? (wrow >> 6) * 32 + (wrow & 31) : wrow;
+      w_off[h][q] = (uint32_t)((int64_t)min(ch, p.N - 1 - n0) * (GATED && h ? p.w_pitch1 : p.w_pitch0)) + wchunk;
     }
+  const int rest = (int)(p.kb % BKB), nk = (int)(p.kb / BKB) + (rest ? 1 : 0);
+  auto k_of = [&](int s) { return (uint32_t)(rest ? (s - 1) * BKB + rest : s * BKB); };
+  auto issue = [&](int s, int h) {
+    const uint32_t k = k_of(s);
+    uint8_t* sb = rows_lds + (s & 1) * Cfg::STAGE_BYTES;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) load_rows_to_lds(xr, x_off[h][q], k, sb + x_blk[h][q] * 1024);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) load_rows_to_lds(h ? w1r : w0r, w_off[h][q], k, sb + w_blk[h][q] * 1024);
+  };
+
+  typename E::Acc16 acc[4][8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[j][i][r] = 0;
+
+  // fragments: x[h][i][g]: rows h * 64 + i * 16 .., w[h][j][g]: channels h * 32 + j * 16 ..; g: 64 bytes of k
+  v4i_b x[2][4][2], w[2][2][2];
+  int cp[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) cp[g] = ((4 * g + quarter) ^ ((l16 >> 1) & 7)) * 16;
+  const int x_row = (wm * 128 + l16) * BKB, w_row = (BM + wn * 64 + l16) * BKB;
+  auto read_x = [&](int s, int h) {
+    const uint8_t* sb = rows_lds + (s & 1) * Cfg::STAGE_BYTES + x_row + h * 64 * BKB;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[h][i][g] = *reinterpret_cast<const v4i_b*>(sb + i * 16 * BKB + cp[g]);
+  };
+  auto read_w = [&](int s, int h) {
+    const uint8_t* sb = rows_lds + (s & 1) * Cfg::STAGE_BYTES + w_row + h * 32 * BKB;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) w[h][j][g] = *reinterpret_cast<const v4i_b*>(sb + j * 16 * BKB + cp[g]);
+  };
+  auto mma = [&](int hx, int hw) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[2 * hw + j][4 * hx + i] = E::mma16(w[hw][j][g], x[hx][i][g], acc[2 * hw + j][4 * hx + i]);
+  };
+
+  // the first stage, through registers if it is what is left of k over whole stages (zeros behind it), and the second
+  if (rest) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int xk = (slot ^ (((x_blk[h][q] * 8 + sub) >> 1) & 7)) * 16, wk = (slot ^ (((w_blk[h][q] * 8 + sub) >> 1) & 7)) * 16;
+        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+        if (xk < rest) a = *reinterpret_cast<const uint4*>(p.x + (int64_t)m0 * p.x_pitch + x_off[h][q]);
+        if (wk < rest) b = *reinterpret_cast<const uint4*>((GATED && h ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0) + w_off[h][q]);
+        *reinterpret_cast<uint4*>(rows_lds + x_blk[h][q] * 1024 + lane * 16) = a;
+        *reinterpret_cast<uint4*>(rows_lds + w_blk[h][q] * 1024 + lane * 16) = b;
+      }
+  } else {
+    issue(0, 0);
+    issue(0, 1);
   }
+  if (nk > 1) {
+    issue(1, 0);
+    issue(1, 1);
+    wait_vmcnt<8>();
+  } else {
+    wait_vmcnt<0>();
+  }
+  lds_handover();
+  read_x(0, 0);
+  read_w(0, 0);
+  lds_handover();
+  // steady: stages s + 1 and s + 2 exist.  The loads outstanding behind the half a wait is for are those of two steps.
+  auto stage = [&](int s, auto steady_c) {
+    constexpr bool steady = decltype(steady_c)::value;
+    if constexpr (steady) issue(s + 2, 0);
+    read_w(s, 1);
+    mma(0, 0);
+    read_x(s, 1);
+    mma(0, 1);
+    sched_pairs<0x100, 4, 1>();
+    sched_pairs<0x010, 4, 1>();
+    sched_mfma<8>();
+    sched_pairs<0x100, 8, 1>();
+    sched_mfma<8>();
+    if constexpr (steady) wait_vmcnt<8>();
+    else wait_vmcnt<4>();
+    lds_handover();
+    if constexpr (steady) issue(s + 2, 1);
+    if (steady || s + 1 < nk) read_x(s + 1, 0);
+    mma(1, 0);
+    if (steady || s + 1 < nk) read_w(s + 1, 0);
+    mma(1, 1);
+    sched_pairs<0x010, 4, 1>();
+    sched_pairs<0x100, 8, 1>();
+    sched_mfma<4>();
+    sched_pairs<0x100, 4, 1>();
+    sched_mfma<12>();
+    if constexpr (steady) wait_vmcnt<8>();
+    else wait_vmcnt<0>();
+    lds_handover();
+  };
+  int s = 0;
+  for (; s + 2 < nk; ++s) stage(s, std::true_type());
+  for (; s < nk; ++s) stage(s, std::false_type());
+  rows_epilogue<E, Cfg>(epi, acc, rows_lds, m0, n0, M);
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------

@@ -222,13 +222,14 @@ __global__ __launch_bounds__(256) void transpose16_kernel(const uint16_t* __rest
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
-typedef RowsCfg<256, 256, 2, 4, 128, 2> Rows256;
 typedef RowsCfg<128, 128, 2, 2, 128, 2> Rows128;
 typedef RowsCfg<64, 128, 2, 2, 128, 3> Rows64;
 
 template <class E, class Cfg, class Epi>
 static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st) {
-  auto kern = gemm_rows_kernel<E, Cfg, Epi>;
+  void (*kern)(RowsProduct, int, int, Epi);
+  if constexpr (std::is_same<Cfg, Rows256>::value) kern = gemm_rows_big_kernel<E, Epi>;
+  else kern = gemm_rows_kernel<E, Cfg, Epi>;
   static std::atomic<uint64_t> ready{0};   // devices whose limit of dynamic LDS has been raised for this kernel
   int dev = 0;
   hipError_t err = hipGetDevice(&dev);

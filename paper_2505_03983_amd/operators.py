@@ -1,8 +1,6 @@
 """The operators of a gated residual network (include/asd.h) on torch tensors: shapes, types and devices are checked here,
 outputs and workspaces are allocated by torch, the kernels run on the tensors' device and its current stream (or `stream`).
 Matrices may have any row pitch; their columns lie next to each other.  There is no fallback: without a GPU a call raises."""
-import ctypes as C
-
 import torch
 
 from . import binding
@@ -10,34 +8,34 @@ from . import binding
 _TYPE = {torch.float32: binding.ASD_F32, torch.bfloat16: binding.ASD_BF16, torch.float16: binding.ASD_F16,
          torch.int8: binding.ASD_I8}
 _ACT = {"silu": binding.ASD_ACT_SILU, "gelu": binding.ASD_ACT_GELU}
-_lib = None
+_entries = {}
 
 
 def _entry(name):
-    global _lib
-    if _lib is None:
-        _lib = binding.lib()
-    return getattr(_lib, name)
+    f = _entries.get(name)
+    if f is None:
+        f = _entries[name] = getattr(binding.lib(), name)
+    return f
 
 
 def _refuse(message):
     raise binding.AsdError(binding.ASD_EINVAL, message)
 
 
-def _matrix(t, name, dtype, device, shape):
+def _matrix(t, name, dtype, device, rows, cols):
     """Address and row pitch of a matrix argument."""
-    if t.dim() != 2 or tuple(t.shape) != shape:
-        _refuse("%s has shape %s, not %s" % (name, tuple(t.shape), shape))
+    if t.shape != (rows, cols):
+        _refuse("%s has shape %s, not %s" % (name, tuple(t.shape), (rows, cols)))
     if t.dtype != dtype:
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
     row, col = t.stride()
-    if shape[1] > 1 and col != 1:
+    if col != 1 and cols > 1:
         _refuse("the columns of %s do not lie next to each other" % name)
-    if shape[0] <= 1:
-        row = shape[1]
-    elif row < shape[1]:
+    if rows <= 1:
+        row = cols
+    elif row < cols:
         _refuse("the rows of %s overlap" % name)
     return t.data_ptr(), row
 
@@ -45,7 +43,7 @@ def _matrix(t, name, dtype, device, shape):
 def _vector(t, name, dtype, device, n):
     if t is None:
         return None
-    if t.dim() != 1 or t.shape[0] != n:
+    if t.shape != (n,):
         _refuse("%s has shape %s, not (%d,)" % (name, tuple(t.shape), n))
     if t.dtype != dtype:
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
@@ -58,9 +56,7 @@ def _vector(t, name, dtype, device, n):
 
 def _new(out, shape, dtype, device):
     """An output argument, or a new array."""
-    if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    return out
+    return torch.empty(shape, dtype=dtype, device=device) if out is None else out
 
 
 def _rows_of(x, name="x"):
@@ -73,21 +69,26 @@ def _rows_of(x, name="x"):
 
 def _launch(name, args, device, stream, workspace=True):
     """Runs an entry on the tensors' device; its workspace is torch's, which hands memory on in the order of the stream."""
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif getattr(stream, "device", device) != device:
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _launch(name, args, device, stream, workspace)
+    if stream is not None and getattr(stream, "device", device) != device:
         _refuse("the stream is on %s, the tensors on %s" % (stream.device, device))
-    with torch.cuda.device(device):
-        ws = None
-        if workspace:
-            need = _entry(name + "_workspace")(args)
-            if need:
+    ws = None
+    if workspace:
+        need = _entry(name + "_workspace")(args)
+        if need:
+            if stream is None:
+                ws = torch.empty(need, dtype=torch.uint8, device=device)
+            else:
                 with torch.cuda.stream(stream):
                     ws = torch.empty(need, dtype=torch.uint8, device=device)
-                args.workspace, args.workspace_bytes = ws.data_ptr(), need
-        s = _entry(name)(args, C.c_void_p(stream.cuda_stream))
-        if s != binding.ASD_OK:
-            raise binding.AsdError(s, binding.last_error())
+            args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    # (the raw handle: the stream object that torch.cuda.current_stream makes takes longer than a launch)
+    raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+    s = _entry(name)(args, raw)
+    if s != binding.ASD_OK:
+        raise binding.AsdError(s, binding.last_error())
 
 
 def rms_norm(x, gain=None, eps=1e-6, residual=None, out_type=None, out=None, scale=None, sum_out=None, rows_used=None,
@@ -101,16 +102,16 @@ def rms_norm(x, gain=None, eps=1e-6, residual=None, out_type=None, out=None, sca
     if t not in _TYPE or out_type not in _TYPE:
         _refuse("no such type: %s -> %s" % (t, out_type))
     a = binding.asd_norm(rows=rows, cols=cols, type=_TYPE[t], out_type=_TYPE[out_type], eps=eps)
-    a.x, a.ld_x = _matrix(x, "x", t, dev, (rows, cols))
+    a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
     out = _new(out, (rows, cols), out_type, dev)
-    a.out, a.ld_out = _matrix(out, "out", out_type, dev, (rows, cols))
+    a.out, a.ld_out = _matrix(out, "out", out_type, dev, rows, cols)
     a.gain = _vector(gain, "gain", t, dev, cols)
     if residual is not None:
-        a.residual, a.ld_residual = _matrix(residual, "residual", t, dev, (rows, cols))
+        a.residual, a.ld_residual = _matrix(residual, "residual", t, dev, rows, cols)
         if sum_out is None:
             sum_out = torch.empty((rows, cols), dtype=t, device=dev)
     if sum_out is not None:
-        a.sum, a.ld_sum = _matrix(sum_out, "sum_out", t, dev, (rows, cols))
+        a.sum, a.ld_sum = _matrix(sum_out, "sum_out", t, dev, rows, cols)
     if out_type == torch.int8:
         scale = _new(scale, (rows,), torch.float32, dev)
         a.scale = _vector(scale, "scale", torch.float32, dev, rows)
@@ -128,9 +129,9 @@ def quantize_rows(x, out=None, scale=None, rows_used=None, stream=None):
     if t not in _TYPE:
         _refuse("no such type: %s" % t)
     a = binding.asd_norm(rows=rows, cols=cols, type=_TYPE[t], out_type=binding.ASD_I8)
-    a.x, a.ld_x = _matrix(x, "x", t, dev, (rows, cols))
+    a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
     out = _new(out, (rows, cols), torch.int8, dev)
-    a.out, a.ld_out = _matrix(out, "out", torch.int8, dev, (rows, cols))
+    a.out, a.ld_out = _matrix(out, "out", torch.int8, dev, rows, cols)
     scale = _new(scale, (rows,), torch.float32, dev)
     a.scale = _vector(scale, "scale", torch.float32, dev, rows)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
@@ -146,13 +147,13 @@ def rms_norm_backward(dy, total, gain=None, eps=1e-6, dsum=None, dx=None, dgain=
     if t not in _TYPE:
         _refuse("no such type: %s" % t)
     a = binding.asd_norm_grad(rows=rows, cols=cols, type=_TYPE[t], eps=eps)
-    a.sum, a.ld_sum = _matrix(total, "total", t, dev, (rows, cols))
-    a.dy, a.ld_dy = _matrix(dy, "dy", t, dev, (rows, cols))
+    a.sum, a.ld_sum = _matrix(total, "total", t, dev, rows, cols)
+    a.dy, a.ld_dy = _matrix(dy, "dy", t, dev, rows, cols)
     if dsum is not None:
-        a.dsum, a.ld_dsum = _matrix(dsum, "dsum", t, dev, (rows, cols))
+        a.dsum, a.ld_dsum = _matrix(dsum, "dsum", t, dev, rows, cols)
     a.gain = _vector(gain, "gain", t, dev, cols)
     dx = _new(dx, (rows, cols), t, dev)
-    a.dx, a.ld_dx = _matrix(dx, "dx", t, dev, (rows, cols))
+    a.dx, a.ld_dx = _matrix(dx, "dx", t, dev, rows, cols)
     dgain = _new(dgain, (cols,), t, dev)
     a.dgain = _vector(dgain, "dgain", t, dev, cols)
     _launch("asd_rms_norm_backward", a, dev, stream)
@@ -167,13 +168,13 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, out_type=torch.bfloat16, out=No
     if out_type not in _TYPE:
         _refuse("no such type: %s" % out_type)
     a = binding.asd_linear8(rows=rows, cols=cols, channels=channels, out_type=_TYPE[out_type])
-    a.x, a.ld_x = _matrix(x, "x", torch.int8, dev, (rows, cols))
-    a.w, a.ld_w = _matrix(w, "w", torch.int8, dev, (channels, cols))
+    a.x, a.ld_x = _matrix(x, "x", torch.int8, dev, rows, cols)
+    a.w, a.ld_w = _matrix(w, "w", torch.int8, dev, channels, cols)
     a.x_scale = _vector(x_scale, "x_scale", torch.float32, dev, rows)
     a.w_scale = _vector(w_scale, "w_scale", torch.float32, dev, channels)
     a.bias = _vector(bias, "bias", torch.float32, dev, channels)
     out = _new(out, (rows, channels), out_type, dev)
-    a.out, a.ld_out = _matrix(out, "out", out_type, dev, (rows, channels))
+    a.out, a.ld_out = _matrix(out, "out", out_type, dev, rows, channels)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
     _launch("asd_linear_i8", a, dev, stream)
     return out
@@ -188,9 +189,9 @@ def _gated_args(x, w_gate, w_up, act, out_type):
         _refuse("unknown activation %r" % (act,))
     channels = w_gate.shape[0] if w_gate.dim() == 2 else 0
     a = binding.asd_gated(rows=rows, cols=cols, channels=channels, type=_TYPE[t], out_type=_TYPE[out_type], act=_ACT[act])
-    a.x, a.ld_x = _matrix(x, "x", t, dev, (rows, cols))
-    a.w_gate, a.ld_w_gate = _matrix(w_gate, "w_gate", t, dev, (channels, cols))
-    a.w_up, a.ld_w_up = _matrix(w_up, "w_up", t, dev, (channels, cols))
+    a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
+    a.w_gate, a.ld_w_gate = _matrix(w_gate, "w_gate", t, dev, channels, cols)
+    a.w_up, a.ld_w_up = _matrix(w_up, "w_up", t, dev, channels, cols)
     return a
 
 
@@ -206,7 +207,7 @@ def gated_ff(x, w_gate, w_up, act="silu", x_scale=None, gate_scale=None, up_scal
         a.gate_scale = _vector(gate_scale, "gate_scale", torch.float32, dev, a.channels)
         a.up_scale = _vector(up_scale, "up_scale", torch.float32, dev, a.channels)
     out = _new(out, (a.rows, a.channels), out_type, dev)
-    a.out, a.ld_out = _matrix(out, "out", out_type, dev, (a.rows, a.channels))
+    a.out, a.ld_out = _matrix(out, "out", out_type, dev, a.rows, a.channels)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
     _launch("asd_gated_ff", a, dev, stream)
     return out
@@ -217,17 +218,17 @@ def gated_ff_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=Tru
     """(dx, dw_gate, dw_up) from dh, the gradient of gated_ff's result; None for what is not needed."""
     a = _gated_args(x, w_gate, w_up, act, x.dtype)
     dev, t = x.device, x.dtype
-    a.dh, a.ld_dh = _matrix(dh, "dh", t, dev, (a.rows, a.channels))
+    a.dh, a.ld_dh = _matrix(dh, "dh", t, dev, a.rows, a.channels)
     if need_dx:
         dx = _new(dx, (a.rows, a.cols), t, dev)
-        a.dx, a.ld_dx = _matrix(dx, "dx", t, dev, (a.rows, a.cols))
+        a.dx, a.ld_dx = _matrix(dx, "dx", t, dev, a.rows, a.cols)
     else:
         dx = None
     if need_dw:
         dw_gate = _new(dw_gate, (a.channels, a.cols), t, dev)
         dw_up = _new(dw_up, (a.channels, a.cols), t, dev)
-        a.dw_gate, a.ld_dw_gate = _matrix(dw_gate, "dw_gate", t, dev, (a.channels, a.cols))
-        a.dw_up, a.ld_dw_up = _matrix(dw_up, "dw_up", t, dev, (a.channels, a.cols))
+        a.dw_gate, a.ld_dw_gate = _matrix(dw_gate, "dw_gate", t, dev, a.channels, a.cols)
+        a.dw_up, a.ld_dw_up = _matrix(dw_up, "dw_up", t, dev, a.channels, a.cols)
     else:
         dw_gate = dw_up = None
     _launch("asd_gated_ff_backward", a, dev, stream)
