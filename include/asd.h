@@ -288,7 +288,7 @@ typedef enum { ASD_ACT_SILU = 0, ASD_ACT_GELU = 1 /* 0.5 z (1 + tanh(sqrt(2/pi) 
  *   out_type ASD_I8: with v = r gain, out = the integer nearest to 127 v / max |v| of the row (ties to even) and
  *   scale[row] (fp32) = max |v| rstd / 127: out * scale is r rstd gain to half a step.  A row of zeros has scale 0; a row that
  *   holds an infinity or a NaN has scale NaN and integers 0.
- *   type (of x, residual, sum, gain): ASD_F32, ASD_BF16 or ASD_F16.  gain [cols], or NULL: 1.  cols <= 65536.
+ *   type (of x, residual, sum, gain): ASD_F32, ASD_BF16 or ASD_F16.  gain [cols], or NULL: 1.  cols <= 32768.
  * asd_quantize_rows: the same without sum and norm: out (int8) = nearest integer to 127 x / max |x|, scale = max |x| / 127.
  *   Uses rows, cols, type, x, ld_x, out, ld_out, scale, rows_used; ignores the other fields. */
 typedef struct {

@@ -140,6 +140,14 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
   constexpr int FACTOR = GATED ? 32 / B : 0;                // blocks from a gate's to the matching up's
   uint8_t* park = lds + wave * (B * ROWB);
   const int col0 = n0 + wn * COLS;                          // channel of the wavefront's first column
+  auto column = [&](int j, int q) { return (GATED ? j * B / 64 * 32 + j * B % 32 : j * B) + (B == 32 ? 8 * q : 0) + 4 * part; };
+  // what belongs to columns is the same for all rows: loaded once
+  typename Epi::Cols cc[NB][RUNS];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int q = 0; q < RUNS; ++q)
+      if (!(GATED && (j * B / 32) % 2)) cc[j][q] = epi.cols(col0 + column(j, q));
   for (int out = 0; out < Epi::kOutputs; ++out) {
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
@@ -152,7 +160,7 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
         if (GATED && (j * B / 32) % 2) continue;
 #pragma unroll
         for (int q = 0; q < RUNS; ++q) {
-          const int c = (GATED ? j * B / 64 * 32 + j * B % 32 : j * B) + (B == 32 ? 8 * q : 0) + 4 * part;
+          const int c = column(j, q);
           typename E::Sum a[4], b[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -160,13 +168,22 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
             b[r] = acc[j + FACTOR][i][4 * q + r];
           }
           Out v[4];
-          epi.values(out, rc, m, col0 + c, a, b, v);
+          epi.values(out, rc, cc[j][q], m, col0 + c, a, b, v);
           const int byte = c * OB, sl = (byte >> 4) ^ (lrow & (SL - 1));
           if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + lrow * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v);
           else *reinterpret_cast<uint4*>(park + lrow * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v);
         }
       }
       // (the region is this wavefront's own, whose LDS operations complete in order)
+      if (!epi.wide) {   // rows at no multiple of 16 bytes: number by number, neighbours by neighbouring lanes
+#pragma unroll 4
+        for (int e = lane; e < B * COLS; e += 64) {
+          const int r = e / COLS, byte = e % COLS * OB;
+          const Out v = *reinterpret_cast<const Out*>(park + r * ROWB + (((byte >> 4) ^ (r & (SL - 1))) * 16) + (byte & 15));
+          if (mrow + r < M) epi.store1(mrow + r, col0 + e % COLS, v);
+        }
+        continue;
+      }
       constexpr int RPI = 64 / SL < B ? 64 / SL : B;        // rows a pass of the wavefront covers
 #pragma unroll
       for (int r0 = 0; r0 < B; r0 += RPI) {

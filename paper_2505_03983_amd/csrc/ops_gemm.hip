@@ -11,11 +11,11 @@
 namespace asd {
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
-// A run of 16 bytes of results, columns n .. of row m of a matrix with n_cols columns.
+// A run of 16 bytes of results, columns n .. of a row of n_cols that starts on 16 bytes.
 template <class T>
-__device__ __forceinline__ void store_cols(T* row, int n, int n_cols, bool wide, uint4 v) {
+__device__ __forceinline__ void store_cols(T* row, int n, int n_cols, uint4 v) {
   constexpr int CNT = 16 / (int)sizeof(T);
-  if (wide && n + CNT <= n_cols) {
+  if (n + CNT <= n_cols) {
     *reinterpret_cast<uint4*>(row + n) = v;
     return;
   }
@@ -39,13 +39,20 @@ struct SumEpi {
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
-  __device__ __forceinline__ void values(int, Row, int, int, const float* a, const float*, T* v) const {
+  struct Cols {};
+  __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
+  __device__ __forceinline__ void values(int, Row, Cols, int, int, const float* a, const float*, T* v) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = (T)a[r];
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const {
-    if (m < first_rows) store_cols(out + m * ld, n, N, wide, v);
-    else if (m >= second && m < second + first_rows) store_cols(out2 + (m - second) * ld2, n, N, wide, v);
+    if (m < first_rows) store_cols(out + m * ld, n, N, v);
+    else if (m >= second && m < second + first_rows) store_cols(out2 + (m - second) * ld2, n, N, v);
+  }
+  __device__ __forceinline__ void store1(int m, int n, T v) const {
+    if (n >= N) return;
+    if (m < first_rows) out[m * ld + n] = v;
+    else if (m >= second && m < second + first_rows) out2[(m - second) * ld2 + n] = v;
   }
   __device__ __forceinline__ void one(int m, int n, float a, float) const {
     if (m < first_rows) out[m * ld + n] = (T)a;
@@ -66,17 +73,28 @@ struct Scaled8Epi {
   typedef T Out;
   static constexpr bool kGated = false;
   static constexpr int kOutputs = 1;
+  struct Cols {
+    float s[4], b[4];
+  };
   __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
-  __device__ __forceinline__ float value(float xs, int n, int a) const {
-    const float v = (float)a * xs * w_scale[n];
-    return bias ? v + bias[n] : v;
-  }
-  __device__ __forceinline__ void values(int, float xs, int, int n, const int* a, const int*, T* v) const {
+  __device__ __forceinline__ Cols cols(int n) const {
+    Cols c;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (T)value(xs, min(n + r, N - 1), a[r]);
+    for (int r = 0; r < 4; ++r) {
+      c.s[r] = w_scale[min(n + r, N - 1)];
+      c.b[r] = bias ? bias[min(n + r, N - 1)] : 0.f;
+    }
+    return c;
   }
-  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, wide, v); }
-  __device__ __forceinline__ void one(int m, int n, int a, int) const { out[m * ld + n] = (T)value(x_scale[m], n, a); }
+  __device__ __forceinline__ void values(int, float xs, const Cols& c, int, int, const int* a, const int*, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (T)((float)a[r] * xs * c.s[r] + c.b[r]);
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
+  __device__ __forceinline__ void store1(int m, int n, T v) const {
+    if (n < N) out[m * ld + n] = v;
+  }
+  __device__ __forceinline__ void one(int m, int n, int a, int) const { out[m * ld + n] = (T)((float)a * x_scale[m] * w_scale[n] + (bias ? bias[n] : 0.f)); }
 };
 
 // Activations and their derivatives, in fp32.  exp2 and the reciprocal are the hardware's (1 ulp each): about 1e-6 of the value,
@@ -109,11 +127,16 @@ struct GatedEpi {
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
-  __device__ __forceinline__ void values(int, Row, int, int, const float* g, const float* u, T* v) const {
+  struct Cols {};
+  __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
+  __device__ __forceinline__ void values(int, Row, Cols, int, int, const float* g, const float* u, T* v) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = (T)(act_value(act, g[r]) * u[r]);
   }
-  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, wide, v); }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
+  __device__ __forceinline__ void store1(int m, int n, T v) const {
+    if (n < N) out[m * ld + n] = v;
+  }
   __device__ __forceinline__ void one(int m, int n, float g, float u) const { out[m * ld + n] = (T)(act_value(act, g) * u); }
 };
 
@@ -129,16 +152,31 @@ struct Gated8Epi {
   typedef T Out;
   static constexpr bool kGated = true;
   static constexpr int kOutputs = 1;
+  struct Cols {
+    float g[4], u[4];
+  };
   __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
-  __device__ __forceinline__ T value(float xs, int n, int g, int u) const {
-    return (T)(act_value(act, (float)g * xs * gate_scale[n]) * ((float)u * xs * up_scale[n]));
-  }
-  __device__ __forceinline__ void values(int, float xs, int, int n, const int* g, const int* u, T* v) const {
+  __device__ __forceinline__ Cols cols(int n) const {
+    Cols c;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = value(xs, min(n + r, N - 1), g[r], u[r]);
+    for (int r = 0; r < 4; ++r) {
+      c.g[r] = gate_scale[min(n + r, N - 1)];
+      c.u[r] = up_scale[min(n + r, N - 1)];
+    }
+    return c;
   }
-  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, wide, v); }
-  __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(x_scale[m], n, g, u); }
+  __device__ __forceinline__ T value(float xs, float gs, float us, int g, int u) const {
+    return (T)(act_value(act, (float)g * xs * gs) * ((float)u * xs * us));
+  }
+  __device__ __forceinline__ void values(int, float xs, const Cols& c, int, int, const int* g, const int* u, T* v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = value(xs, c.g[r], c.u[r], g[r], u[r]);
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
+  __device__ __forceinline__ void store1(int m, int n, T v) const {
+    if (n < N) out[m * ld + n] = v;
+  }
+  __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(x_scale[m], gate_scale[n], up_scale[n], g, u); }
 };
 
 // dg = dh u act'(g) and du = dh act(g), side by side: dgu [rows][2 Np], zeros in the columns N .. Np - 1 of either half.  Rounded
@@ -150,20 +188,33 @@ struct GatedGradEpi {
   const T* dh;
   int64_t ld_dh;
   int N, act;
+  bool dh_wide;   // runs of four of dh lie on 8 bytes
   typedef T Out;
   static constexpr bool kGated = true;
   static constexpr int kOutputs = 2;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
-  __device__ __forceinline__ void values(int which, Row, int m, int n, const float* g, const float* u, T* v) const {
+  struct Cols {};
+  __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
+  __device__ __forceinline__ void values(int which, Row, Cols, int m, int n, const float* g, const float* u, T* v) const {
+    T dv[4];
+    const T* at = dh + m * ld_dh + n;
+    if (dh_wide && n + 4 <= N) {
+      *reinterpret_cast<uint2*>(dv) = *reinterpret_cast<const uint2*>(at);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) dv[r] = n + r < N ? at[r] : (T)0.f;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float d = n + r < N ? (float)dh[m * ld_dh + n + r] : 0.f;
+      const float d = (float)dv[r];
       float value, slope;
       act_both(act, g[r], &value, &slope);
       v[r] = n + r < N ? (T)(which ? d * value : d * u[r] * slope) : (T)0.f;
     }
   }
+  static constexpr bool wide = true;
+  __device__ __forceinline__ void store1(int, int, T) const {}
   __device__ __forceinline__ void store(int which, int m, int n, uint4 v) const {
     if (n < Np) *reinterpret_cast<uint4*>(dgu + (int64_t)m * 2 * Np + which * Np + n) = v;
   }
@@ -179,9 +230,19 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const uint8_t* __restric
   if (row >= rows) return;
   const uint8_t* s = src + row * pitch + k;
   uint32_t v[4] = {0u, 0u, 0u, 0u};
+  if (k > 0 && k + 20 <= bytes) {   // five words around the sixteen bytes, all of this row
+    const int shift = (int)((uintptr_t)s & 3);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(s - shift);
+    uint32_t a[5];
 #pragma unroll
-  for (int b = 0; b < 16; ++b)
-    if (k + b < bytes) v[b >> 2] |= (uint32_t)s[b] << (8 * (b & 3));
+    for (int i = 0; i < 5; ++i) a[i] = w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(a[i + 1], a[i], shift);
+  } else {
+#pragma unroll
+    for (int b = 0; b < 16; ++b)
+      if (k + b < bytes) v[b >> 2] |= (uint32_t)s[b] << (8 * (b & 3));
+  }
   *reinterpret_cast<uint4*>(dst + at) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
@@ -222,8 +283,8 @@ __global__ __launch_bounds__(256) void transpose16_kernel(const uint16_t* __rest
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
-typedef RowsCfg<128, 128, 2, 2, 128, 2> Rows128;
-typedef RowsCfg<64, 128, 2, 2, 128, 3> Rows64;
+typedef RowsCfg<128, 128, 2, 2, 128, 4> Rows128;
+typedef RowsCfg<64, 128, 2, 2, 128, 5> Rows64;
 
 template <class E, class Cfg, class Epi>
 static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st) {
@@ -245,24 +306,62 @@ static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st
   return hipGetLastError();
 }
 
+// Which kernel: the least of the estimates below, in microseconds.  A tile takes f + k per 128 bytes of k, a workgroup has its CU
+// to itself, and from the third round on the CUs no longer finish together.  Fitted to 24 .. 2000 rows by 1024 .. 11000 channels of
+// 1024 .. 11008 numbers, 8-bit products and bf16 gated units (both matrices' channels count), operands from the Infinity Cache.
+// Few rows: the weights' bytes at a rate that falls with the rows a workgroup holds, each 64 rows reading them again.
+// Measured, few / 64 x 128 / 128 x 128 / 256 x 256: 8 bits, 4096 channels of 4096: 8 rows 7.1 / 12.4 / 13.8 / -, 64 rows 13.6 / 12.6 /
+// 14.9 / -, 1000 rows - / 28 / 23 / 47, 4000 rows - / 110 / 83 / 59; gated bf16, 4096 channels of 4096: 8 rows 18 / 20 / 23 / -, 64 rows
+// 31 / 20 / 24 / -, 400 rows - / 42 / 32 / 82, 2000 rows - / 177 / 129 / 108.  Of those 80 calls the rule misses the fastest kernel
+// by more than a tenth in two.
+struct RowsCost {
+  int bm, bn;
+  float f, k;
+  float full;   // a tile takes this much longer where there are more tiles than CUs
+};
+constexpr RowsCost kRowsCost[3] = {{256, 256, 8.f, 1.14f, 1.15f}, {128, 128, 4.5f, 0.34f, 1.3f}, {64, 128, 4.5f, 0.27f, 1.1f}};
 constexpr int kFewRows = 64;
+constexpr float kFewRate[3] = {4.6f, 2.9f, 1.8f};   // TB/s; up to 16, 32, 64 rows
+
+// 0 .. 2: a tile; 3 .. 5: few rows, 16 .. 64 at a time
+static int pick_product(int M, int64_t n, int64_t kb) {
+  int best = 0;
+  float least = INFINITY;
+  for (int i = 0; i < 3; ++i) {
+    const RowsCost& c = kRowsCost[i];
+    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(n, c.bn);
+    float rounds = (float)ceil_div(tiles, 256);
+    if (rounds > 2.f) rounds = 0.4f * rounds + 0.6f * (float)tiles / 256.f;
+    const float t = rounds * (tiles > 256 ? c.full : 1.f) * (c.f + c.k * (float)ceil_div(kb, 128));
+    if (t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  if (M <= kFewRows) {
+    const int few = M <= 16 ? 0 : M <= 32 ? 1 : 2;
+    if (3.f + 1e-6f * (float)n * (float)kb / kFewRate[few] < least) best = 3 + few;
+  }
+  return best;
+}
+
+template <class E, int MT, class Epi>
+static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)ceil_div(p.M, 16 * MT));
+  hipLaunchKernelGGL((gemm_few_rows_kernel<E, MT, Epi>), grid, dim3(512), 0, st, p, e);
+  return hipGetLastError();
+}
 
 template <class E, class Epi>
 static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st) {
+  const int pick = pick_product(p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
   if constexpr (Epi::kOutputs == 1) {
-    if (p.M <= kFewRows) {
-      const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
-      const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)ceil_div(p.M, 16 * mt));
-      if (mt == 1) hipLaunchKernelGGL((gemm_few_rows_kernel<E, 1, Epi>), grid, dim3(512), 0, st, p, e);
-      else if (mt == 2) hipLaunchKernelGGL((gemm_few_rows_kernel<E, 2, Epi>), grid, dim3(512), 0, st, p, e);
-      else hipLaunchKernelGGL((gemm_few_rows_kernel<E, 4, Epi>), grid, dim3(512), 0, st, p, e);
-      return hipGetLastError();
-    }
+    if (pick == 3) return launch_few<E, 1>(p, e, st);
+    if (pick == 4) return launch_few<E, 2>(p, e, st);
+    if (pick == 5) return launch_few<E, 4>(p, e, st);
   }
-  const int64_t n = Epi::kGated ? 2 * (int64_t)p.N : p.N;
-  if (ceil_div(p.M, 256) * ceil_div(n, 256) >= 192) return launch_rows<E, Rows256>(p, e, st);
-  if (ceil_div(p.M, 128) * ceil_div(n, 128) >= 256) return launch_rows<E, Rows128>(p, e, st);
-  return launch_rows<E, Rows64>(p, e, st);
+  if (pick == 0) return launch_rows<E, Rows256>(p, e, st);
+  return pick == 1 ? launch_rows<E, Rows128>(p, e, st) : launch_rows<E, Rows64>(p, e, st);
 }
 
 constexpr int64_t kMaxPitch = (int64_t)4 << 20;   // bytes: a tile's offsets stay within 32 bits
@@ -418,7 +517,8 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   ASD_HIP(bring(o.in.g, st));
   ASD_HIP(bring(o.in.u, st));
   T* dgu = reinterpret_cast<T*>(o.dgu);
-  const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act};
+  const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act,
+                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0};
   ASD_HIP(launch_product<E>(gated_product(p, o.in), e, st));
   if (p.dx) {
     ASD_HIP(transpose16(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, 2 * o.Np, st));

@@ -20,48 +20,37 @@ namespace asd {
 
 constexpr int kRun = 8;   // numbers a thread loads at once
 
-// Numbers a thread holds of a row: its c-th run of eight, or (wide false) eight single ones, `threads` apart.
+// Numbers a thread holds of a row, in the row's own type: its c-th run of eight (WIDE: rows of whole runs on multiples of 16
+// bytes), or eight single ones, `threads` apart.
 template <class T>
-__device__ __forceinline__ void load_run(const T* row, int cols, int threads, int t, bool wide, int c, float* v) {
-  const int first = (c * threads + t) * kRun;
-  if (wide && first + kRun <= cols) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = *reinterpret_cast<const float4*>(row + first), b = *reinterpret_cast<const float4*>(row + first + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      T h[kRun];
-      *reinterpret_cast<uint4*>(h) = *reinterpret_cast<const uint4*>(row + first);
+struct __attribute__((aligned(sizeof(T) == 1 ? 8 : 16))) Run {
+  T v[kRun];
+};
+template <bool WIDE, class T>
+__device__ __forceinline__ void fetch_run(const T* row, int cols, int threads, int t, int c, Run<T>& v) {
+  if constexpr (WIDE) {
+    const int first = (c * threads + t) * kRun;
+    if (first < cols) v = *reinterpret_cast<const Run<T>*>(row + first);
+    else v = Run<T>{};
+  } else {
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) v[k] = (float)h[k];
+    for (int k = 0; k < kRun; ++k) {
+      const int i = (c * kRun + k) * threads + t;
+      v.v[k] = i < cols ? row[i] : (T)0.f;
     }
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < kRun; ++k) {
-    const int i = wide ? first + k : (c * kRun + k) * threads + t;
-    v[k] = i < cols ? (float)row[i] : 0.f;
   }
 }
-
-template <class T>
-__device__ __forceinline__ void store_run(T* row, int cols, int threads, int t, bool wide, int c, const T* v) {
-  const int first = (c * threads + t) * kRun;
-  if (wide && first + kRun <= cols) {
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<uint4*>(row + first) = *reinterpret_cast<const uint4*>(v);
-      *reinterpret_cast<uint4*>(row + first + 4) = *reinterpret_cast<const uint4*>(v + 4);
-    } else if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(row + first) = *reinterpret_cast<const uint4*>(v);
-    } else {
-      *reinterpret_cast<uint2*>(row + first) = *reinterpret_cast<const uint2*>(v);
-    }
-    return;
-  }
+template <bool WIDE, class T>
+__device__ __forceinline__ void store_run(T* row, int cols, int threads, int t, int c, const Run<T>& v) {
+  if constexpr (WIDE) {
+    const int first = (c * threads + t) * kRun;
+    if (first < cols) *reinterpret_cast<Run<T>*>(row + first) = v;
+  } else {
 #pragma unroll
-  for (int k = 0; k < kRun; ++k) {
-    const int i = wide ? first + k : (c * kRun + k) * threads + t;
-    if (i < cols) row[i] = v[k];
+    for (int k = 0; k < kRun; ++k) {
+      const int i = (c * kRun + k) * threads + t;
+      if (i < cols) row[i] = v.v[k];
+    }
   }
 }
 
@@ -103,8 +92,8 @@ __device__ __forceinline__ void row_total(double& a, double& b, double& top, dou
 }
 
 // x, residual, sum and gain of type T; out of type O (int8_t: with scales).  THREADS threads a row, RUNS runs a thread.
-template <class T, class O, int THREADS, int RUNS, bool NORM>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel(asd_norm p, int wide) {
+template <class T, class O, int THREADS, int RUNS, bool NORM, bool WIDE>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel(asd_norm p) {
   constexpr bool I8 = sizeof(O) == 1;
   constexpr int PER_WG = THREADS < 256 ? 256 / THREADS : 1;
   __shared__ double lds[THREADS / 64][3];
@@ -116,34 +105,35 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
   const T* res = NORM && p.residual ? static_cast<const T*>(p.residual) + row * p.ld_residual : nullptr;
   const T* gain = NORM ? static_cast<const T*>(p.gain) : nullptr;
   float r[RUNS][kRun];
+  Run<T> g[RUNS];
+  {
+    Run<T> a[RUNS], b[RUNS];
 #pragma unroll
-  for (int c = 0; c < RUNS; ++c) load_run(x, p.cols, THREADS, t, wide & 1, c, r[c]);
-  if (res) {
-    float q[RUNS][kRun];
+    for (int c = 0; c < RUNS; ++c) fetch_run<WIDE>(x, p.cols, THREADS, t, c, a[c]);
+    if (res)
 #pragma unroll
-    for (int c = 0; c < RUNS; ++c) load_run(res, p.cols, THREADS, t, wide & 1, c, q[c]);
+      for (int c = 0; c < RUNS; ++c) fetch_run<WIDE>(res, p.cols, THREADS, t, c, b[c]);
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      if (gain) fetch_run<WIDE>(gain, p.cols, THREADS, t, c, g[c]);
+      else
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) g[c].v[k] = (T)1.f;
+    }
 #pragma unroll
     for (int c = 0; c < RUNS; ++c)
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) r[c][k] += q[c][k];
+      for (int k = 0; k < kRun; ++k) r[c][k] = res ? (float)a[c].v[k] + (float)b[c].v[k] : (float)a[c].v[k];
   }
   if (NORM && p.sum) {
     T* sum = static_cast<T*>(p.sum) + row * p.ld_sum;
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) {
-      T v[kRun];
+      Run<T> v;
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) v[k] = (T)r[c][k];
-      store_run(sum, p.cols, THREADS, t, wide & 1, c, v);
+      for (int k = 0; k < kRun; ++k) v.v[k] = (T)r[c][k];
+      store_run<WIDE>(sum, p.cols, THREADS, t, c, v);
     }
-  }
-  float g[RUNS][kRun];
-#pragma unroll
-  for (int c = 0; c < RUNS; ++c) {
-    if (gain) load_run(gain, p.cols, THREADS, t, wide & 1, c, g[c]);
-    else
-#pragma unroll
-      for (int k = 0; k < kRun; ++k) g[c][k] = 1.f;
   }
   // odd: NaN as soon as one of the row's v is not a number below infinity
   double squares = 0.0, odd = 0.0, top = 0.0;
@@ -154,7 +144,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
       const double d = (double)r[c][k];
       if constexpr (NORM) squares = fma(d, d, squares);
       if constexpr (I8) {
-        const double v = NORM ? d * (double)g[c][k] : d;
+        const double v = NORM ? d * (double)(float)g[c].v[k] : d;
         odd = fma(v, 0.0, odd);
         top = fmax(top, fabs(v));
       }
@@ -169,108 +159,137 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
     const bool some = good && top > 0.0;
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) {
-      int8_t q[kRun];
+      Run<int8_t> q;
 #pragma unroll
       for (int k = 0; k < kRun; ++k) {
-        const double d = (double)r[c][k], a = 127.0 * (NORM ? d * (double)g[c][k] : d);
+        const double d = (double)r[c][k], a = 127.0 * (NORM ? d * (double)(float)g[c].v[k] : d);
         const double q0 = a * inv, q1 = fma(fma(-q0, top, a), inv, q0);
-        q[k] = some ? (int8_t)(int)rint(q1) : (int8_t)0;
+        q.v[k] = some ? (int8_t)(int)rint(q1) : (int8_t)0;
       }
-      store_run(out, p.cols, THREADS, t, wide & 2, c, q);
+      store_run<WIDE>(out, p.cols, THREADS, t, c, q);
     }
   } else {
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) {
-      O v[kRun];
+      Run<O> v;
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) v[k] = (O)((float)((double)r[c][k] * rstd) * g[c][k]);   // (rstd alone may leave fp32)
-      store_run(out, p.cols, THREADS, t, wide & 2, c, v);
+      for (int k = 0; k < kRun; ++k) v.v[k] = (O)((float)((double)r[c][k] * rstd) * (float)g[c].v[k]);   // (rstd alone may leave fp32)
+      store_run<WIDE>(out, p.cols, THREADS, t, c, v);
     }
   }
 }
 
-// Gradient.  A workgroup takes every gridDim.x-th row, and adds dy n up by column as it goes; the columns' parts, one row of them
-// for each workgroup, are added in their order by the second kernel.
-template <class T, int THREADS, int RUNS>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_grad_kernel(asd_norm_grad p, int wide, float* parts) {
+// Gradient.  A workgroup (or, for short rows, a wavefront) takes every n-th row, fetching the next one while it works, and adds
+// dy n up by column as it goes; the columns' parts, one row of them for each, are added in their order by the second kernel.
+template <class T, int THREADS, int RUNS, bool WIDE>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_grad_kernel(asd_norm_grad p, float* parts) {
   constexpr int PER_WG = THREADS < 256 ? 256 / THREADS : 1;
-  __shared__ double lds[THREADS / 64][3];
+  constexpr bool AHEAD = RUNS * (int)sizeof(T) <= (THREADS == 1024 ? 2 : 6);   // (where registers last)
+  __shared__ double lds[2][THREADS / 64][2];
   const int t = threadIdx.x % THREADS, lane_row = PER_WG > 1 ? (int)threadIdx.x / THREADS : 0;
   const int part = (int)blockIdx.x * PER_WG + lane_row, n_parts = (int)gridDim.x * PER_WG;
-  float g[RUNS][kRun], dg[RUNS][kRun];
-#pragma unroll
-  for (int c = 0; c < RUNS; ++c) {
-    if (p.gain) load_run(static_cast<const T*>(p.gain), p.cols, THREADS, t, wide & 1, c, g[c]);
-#pragma unroll
-    for (int k = 0; k < kRun; ++k) {
-      if (!p.gain) g[c][k] = 1.f;
-      dg[c][k] = 0.f;
-    }
-  }
-  for (int row = part; row < p.rows; row += n_parts) {
-    float r[RUNS][kRun], dy[RUNS][kRun];
+  Run<T> g[RUNS], r[RUNS], dy[RUNS];
+  Run<float> dg[RUNS];
+  auto fetch = [&](int row) {
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) {
-      load_run(static_cast<const T*>(p.sum) + row * p.ld_sum, p.cols, THREADS, t, wide & 1, c, r[c]);
-      load_run(static_cast<const T*>(p.dy) + row * p.ld_dy, p.cols, THREADS, t, wide & 1, c, dy[c]);
+      fetch_run<WIDE>(static_cast<const T*>(p.sum) + row * p.ld_sum, p.cols, THREADS, t, c, r[c]);
+      fetch_run<WIDE>(static_cast<const T*>(p.dy) + row * p.ld_dy, p.cols, THREADS, t, c, dy[c]);
     }
-    double squares = 0.0, along = 0.0, none = 0.0;
+  };
+  if (AHEAD && part < p.rows) fetch(part);
+#pragma unroll
+  for (int c = 0; c < RUNS; ++c) {
+    if (p.gain) fetch_run<WIDE>(static_cast<const T*>(p.gain), p.cols, THREADS, t, c, g[c]);
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      if (!p.gain) g[c].v[k] = (T)1.f;
+      dg[c].v[k] = 0.f;
+    }
+  }
+  int turn = 0;
+  for (int row = part; row < p.rows; row += n_parts) {
+    Run<T> rn[RUNS], dyn[RUNS], ds[RUNS];
+    if (!AHEAD) fetch(row);
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      rn[c] = r[c];
+      dyn[c] = dy[c];
+    }
+    if (p.dx && p.dsum)
+#pragma unroll
+      for (int c = 0; c < RUNS; ++c) fetch_run<WIDE>(static_cast<const T*>(p.dsum) + row * p.ld_dsum, p.cols, THREADS, t, c, ds[c]);
+    if (AHEAD && row + n_parts < p.rows) fetch(row + n_parts);
+    // (a thread's few products in 32 bits, except the squares, which may leave their range)
+    double squares = 0.0;
+    float mine = 0.f;
 #pragma unroll
     for (int c = 0; c < RUNS; ++c)
 #pragma unroll
       for (int k = 0; k < kRun; ++k) {
-        const double d = (double)r[c][k];
-        squares = fma(d, d, squares);
-        along = fma((double)(g[c][k] * dy[c][k]), d, along);
+        const float d = (float)rn[c].v[k];
+        squares = fma((double)d, (double)d, squares);
+        mine = fmaf((float)g[c].v[k] * (float)dyn[c].v[k], d, mine);
       }
-    row_total<THREADS>(squares, along, none, lds);
+    double along = (double)mine;
+    squares = wave_sum64(squares);
+    along = wave_sum64(along);
+    if constexpr (THREADS > 64) {   // (two sets in turn: one barrier a row)
+      if ((threadIdx.x & 63) == 0) {
+        lds[turn][threadIdx.x >> 6][0] = squares;
+        lds[turn][threadIdx.x >> 6][1] = along;
+      }
+      __syncthreads();
+      squares = along = 0.0;
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) {
+        squares += lds[turn][w][0];
+        along += lds[turn][w][1];
+      }
+      turn ^= 1;
+    }
     const double rs = 1.0 / sqrt(squares / (double)p.cols + p.eps);
     const float rstd = (float)rs, mean = (float)(along * rs / (double)p.cols);
 #pragma unroll
-    for (int c = 0; c < RUNS; ++c)
+    for (int c = 0; c < RUNS; ++c) {
+      Run<T> v;
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) r[c][k] = (float)((double)r[c][k] * rs);   // n from here on
-    if (p.dx) {
-      const T* ds = p.dsum ? static_cast<const T*>(p.dsum) + row * p.ld_dsum : nullptr;
-#pragma unroll
-      for (int c = 0; c < RUNS; ++c) {
-        float q[kRun];
-        T v[kRun];
-        if (ds) load_run(ds, p.cols, THREADS, t, wide & 1, c, q);
-#pragma unroll
-        for (int k = 0; k < kRun; ++k) {
-          const float d = rstd * (g[c][k] * dy[c][k] - r[c][k] * mean);
-          v[k] = (T)(ds ? d + q[k] : d);
-        }
-        store_run(static_cast<T*>(p.dx) + row * p.ld_dx, p.cols, THREADS, t, wide & 1, c, v);
+      for (int k = 0; k < kRun; ++k) {
+        const float n = (float)rn[c].v[k] * rstd, y = (float)dyn[c].v[k];
+        const float d = rstd * ((float)g[c].v[k] * y - n * mean);
+        v.v[k] = (T)(p.dsum ? d + (float)ds[c].v[k] : d);
+        dg[c].v[k] = fmaf(y, n, dg[c].v[k]);
       }
+      if (p.dx) store_run<WIDE>(static_cast<T*>(p.dx) + row * p.ld_dx, p.cols, THREADS, t, c, v);
     }
-#pragma unroll
-    for (int c = 0; c < RUNS; ++c)
-#pragma unroll
-      for (int k = 0; k < kRun; ++k) dg[c][k] = fmaf(dy[c][k], r[c][k], dg[c][k]);
   }
   if (parts)
 #pragma unroll
-    for (int c = 0; c < RUNS; ++c) store_run(parts + (int64_t)part * p.cols, p.cols, THREADS, t, (wide & 1) && (p.cols & 3) == 0, c, dg[c]);
+    for (int c = 0; c < RUNS; ++c) store_run<WIDE>(parts + (int64_t)part * p.cols, p.cols, THREADS, t, c, dg[c]);
 }
 
-// dgain: 64 columns a workgroup, its four wavefronts take every fourth part, in order.
+// dgain: 64 columns a workgroup, its sixteen wavefronts take every sixteenth part, in order.
 template <class T>
-__global__ __launch_bounds__(256) void norm_gain_grad_kernel(int cols, int n_parts, const float* __restrict__ parts, T* __restrict__ dgain) {
-  __shared__ float lds[4][64];
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(1024) void norm_gain_grad_kernel(int cols, int n_parts, const float* __restrict__ parts, T* __restrict__ dgain) {
+  __shared__ float lds[16][64];
+  const int lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane, wave = threadIdx.x >> 6;
   float s = 0.f;
   if (col < cols)
 #pragma unroll 8
-    for (int i = wave; i < n_parts; i += 4) s += parts[(int64_t)i * cols + col];
-  lds[wave][threadIdx.x & 63] = s;
+    for (int i = wave; i < n_parts; i += 16) s += parts[(int64_t)i * cols + col];
+  lds[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && col < cols) dgain[col] = (T)((lds[0][threadIdx.x] + lds[1][threadIdx.x]) + (lds[2][threadIdx.x] + lds[3][threadIdx.x]));
+  if (wave == 0 && col < cols) {
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += lds[w][lane];
+    dgain[col] = (T)s;
+  }
 }
 
-// f(threads, runs) as constants for rows of `cols`: the fewest threads that hold one in four runs each (up to 2048 numbers a
-// wavefront, 8192 four, 32768 sixteen), then eight runs.
+// f(threads, runs) as constants for rows of `cols`: a wavefront a row up to 1024 numbers, four up to 6144, sixteen from there.  Few
+// runs a thread leave registers for more rows in flight: 16384 rows of 8192 bf16 numbers with a residual into integers 257 us with
+// four runs in four wavefronts, 233 with one in sixteen.
 template <class F>
 static asd_status by_width(int cols, F f) {
   typedef std::integral_constant<int, 64> W1;
@@ -281,28 +300,25 @@ static asd_status by_width(int cols, F f) {
   if (runs(64) <= 2) return f(W1(), std::integral_constant<int, 2>());
   if (runs(256) <= 1) return f(W4(), std::integral_constant<int, 1>());
   if (runs(256) <= 2) return f(W4(), std::integral_constant<int, 2>());
-  if (runs(256) <= 4) return f(W4(), std::integral_constant<int, 4>());
+  if (runs(256) <= 3) return f(W4(), std::integral_constant<int, 3>());
+  if (runs(1024) <= 1) return f(W16(), std::integral_constant<int, 1>());
   if (runs(1024) <= 2) return f(W16(), std::integral_constant<int, 2>());
-  if (runs(1024) <= 4) return f(W16(), std::integral_constant<int, 4>());
-  return f(W16(), std::integral_constant<int, 8>());
+  return f(W16(), std::integral_constant<int, 4>());
 }
 
-constexpr int kMaxNormCols = 65536;
+constexpr int kMaxNormCols = 32768;
 
 template <class T, class O, bool NORM>
 static asd_status run_norm(const asd_norm& p, hipStream_t st) {
-  int wide = on16(p.x, p.ld_x, sizeof(T)) ? 1 : 0;
-  if (NORM) {
-    if ((p.residual && !on16(p.residual, p.ld_residual, sizeof(T))) || (p.sum && !on16(p.sum, p.ld_sum, sizeof(T))) ||
-        (p.gain && ((uintptr_t)p.gain & 15)))
-      wide = 0;
-  }
-  // (runs of eight int8 are eight bytes; a thread's numbers are the same ones on the way in and out)
-  const bool out_wide = sizeof(O) == 1 ? ((uintptr_t)p.out & 7) == 0 && (p.ld_out & 7) == 0 : on16(p.out, p.ld_out, sizeof(O));
-  wide = wide && out_wide ? 3 : 0;
+  bool wide = p.cols % kRun == 0 && on16(p.x, p.ld_x, sizeof(T)) && ((uintptr_t)p.out & 15) == 0 && p.ld_out % kRun == 0;
+  if (NORM)
+    wide = wide && (!p.residual || on16(p.residual, p.ld_residual, sizeof(T))) && (!p.sum || on16(p.sum, p.ld_sum, sizeof(T))) &&
+           ((uintptr_t)p.gain & 15) == 0;
   return by_width(p.cols, [&](auto threads, auto runs) -> asd_status {
     constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
-    hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM>), dim3((unsigned)ceil_div(p.rows, PER)), dim3(TH * PER), 0, st, p, wide);
+    const dim3 grid((unsigned)ceil_div(p.rows, PER)), block(TH * PER);
+    if (wide) hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM, false>), grid, block, 0, st, p);
     ASD_HIP(hipGetLastError());
     return ASD_OK;
   });
@@ -355,29 +371,30 @@ static asd_status check_norm(const asd_norm* p, bool norm) {
   return check_mats(m, 7, [](int i, int j) { return i == 0 && (j == 3 || j == 4); });
 }
 
-// Parts of dgain: enough workgroups to fill the chip (four of 256 threads a CU), no more than eight rows leave worth a part.
+// Parts of dgain: as many workgroups as are on the chip at a time (two a CU), where each gets eight rows at least.
 static int norm_grad_wgs(int rows, int cols) {
   const int per_wg = cols <= 2 * 64 * kRun ? 4 : 1;   // rows a workgroup takes at a time (by_width)
-  return (int)std::max<int64_t>(1, std::min<int64_t>(1024, ceil_div(rows, 8 * per_wg)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(512, ceil_div(rows, 8 * per_wg)));
 }
 static int norm_grad_parts(int rows, int cols) { return norm_grad_wgs(rows, cols) * (cols <= 2 * 64 * kRun ? 4 : 1); }
 
 template <class T>
 static asd_status run_norm_grad(const asd_norm_grad& p, hipStream_t st) {
-  int wide = on16(p.dy, p.ld_dy, sizeof(T)) && on16(p.sum, p.ld_sum, sizeof(T)) && (!p.gain || ((uintptr_t)p.gain & 15) == 0) &&
+  const bool wide = p.cols % kRun == 0 && on16(p.dy, p.ld_dy, sizeof(T)) && on16(p.sum, p.ld_sum, sizeof(T)) && (!p.gain || ((uintptr_t)p.gain & 15) == 0) &&
              (!p.dsum || on16(p.dsum, p.ld_dsum, sizeof(T))) && (!p.dx || on16(p.dx, p.ld_dx, sizeof(T)));
   float* parts = p.dgain ? static_cast<float*>(p.workspace) : nullptr;
   if (p.rows > 0) {
     ASD_TRY(by_width(p.cols, [&](auto threads, auto runs) -> asd_status {
       constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
-      hipLaunchKernelGGL((rms_norm_grad_kernel<T, TH, R>), dim3((unsigned)norm_grad_wgs(p.rows, p.cols)), dim3(TH * PER), 0, st, p, wide,
-                         parts);
+      const dim3 grid((unsigned)norm_grad_wgs(p.rows, p.cols)), block(TH * PER);
+      if (wide) hipLaunchKernelGGL((rms_norm_grad_kernel<T, TH, R, true>), grid, block, 0, st, p, parts);
+      else hipLaunchKernelGGL((rms_norm_grad_kernel<T, TH, R, false>), grid, block, 0, st, p, parts);
       ASD_HIP(hipGetLastError());
       return ASD_OK;
     }));
   }
   if (p.dgain) {
-    hipLaunchKernelGGL((norm_gain_grad_kernel<T>), dim3((unsigned)ceil_div(p.cols, 64)), dim3(256), 0, st, p.cols,
+    hipLaunchKernelGGL((norm_gain_grad_kernel<T>), dim3((unsigned)ceil_div(p.cols, 64)), dim3(1024), 0, st, p.cols,
                        p.rows > 0 ? norm_grad_parts(p.rows, p.cols) : 0, parts, static_cast<T*>(p.dgain));
     ASD_HIP(hipGetLastError());
   }

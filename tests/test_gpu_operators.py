@@ -68,7 +68,7 @@ def integers(v):
 
 
 WIDTHS = [(1, 1), (3, 2), (1, 64), (5, 7), (4, 512), (7, 513), (6, 1000), (2, 2048), (3, 2056), (5, 4104), (3, 8192), (2, 8193),
-          (3, 16384), (2, 30001), (2, 65536)]
+          (3, 16384), (2, 30001), (2, 32768)]
 
 
 @pytest.mark.parametrize("rows, cols", WIDTHS)
@@ -145,7 +145,7 @@ def test_integers_at_ties_zeros_infinities():
 
 
 @pytest.mark.parametrize("rows, cols", [(1, 1), (3, 5), (40, 64), (33, 1000), (300, 1024), (70, 1032), (17, 4104), (5, 8200),
-                                        (3, 20000), (2, 65536), (9000, 72)])
+                                        (3, 20000), (2, 32768), (9000, 72)])
 @pytest.mark.parametrize("t", [F32, BF16, F16])
 def test_norm_gradient(rows, cols, t):
     g = gen(rows + cols)
@@ -157,9 +157,9 @@ def test_norm_gradient(rows, cols, t):
     n = d * rstd
     along = (gd * dyd * n).mean(1, keepdim=True)
     want = rstd * (gd * dyd - n * along)
-    # each term to a few roundings of fp32 (g dy, rstd, mean, r rstd mean, their difference, the last product and sum); along is
-    # summed in 64 bits from products rounded to fp32
-    slack = 8 * U * rstd * ((gd * dyd).abs() + (n * along).abs() + n.abs() * (gd * dyd * n).abs().mean(1, keepdim=True))
+    # each term to a few roundings of fp32 (g dy, rstd, n, mean, n mean, their difference, the last product and sum); along is
+    # summed in fp32 over up to 32 products of a thread, in 64 bits from there
+    slack = 40 * U * rstd * ((gd * dyd).abs() + (n * along).abs() + n.abs() * (gd * dyd * n).abs().mean(1, keepdim=True))
     for ds in (None, dsum):
         dx, dgain = O().rms_norm_backward(dy, r, gain, EPS, dsum=ds)
         w = want if ds is None else want + ds.double()
