@@ -81,8 +81,37 @@ def mlp_params(d, E, width, n_blocks, K, model_seed=1, out_clip=1.0, predict_eps
     )
 
 
+def _as_i8(a):
+    """Rows (last axis) as 8-bit integers, and their scales."""
+    top = np.abs(a).max(axis=-1, keepdims=True)
+    return np.rint(a * (127.0 / top)).astype(np.int8), (top[..., 0] / 127.0).astype(np.float32)
+
+
+def gated_params(d, E, width, hidden, n_blocks, K, model_seed=1, eight_bit=False, act=0, **kw):
+    """mlp_params with gated blocks: gains near 1 (fp32), weights ~ N(0, 1/fan_in) rounded to bf16 (uint16 patterns), or as 8-bit
+    integers with a scale per output channel."""
+    p = mlp_params(d, E, width, 1, K, model_seed, **kw)
+    for k in ("w_blk", "b_blk"):
+        del p[k]
+    rng = _rng(model_seed, 3)
+    p["gain"] = (1.0 + 0.1 * rng.standard_normal((n_blocks, width))).astype(np.float32)
+    p["block_type"], p["act"], p["eps"] = (3 if eight_bit else 1), int(act), 1e-6
+    for w, scale, shape in (("w_gate", "gate_scale", (n_blocks, hidden, width)), ("w_up", "up_scale", (n_blocks, hidden, width)),
+                            ("w_down", "down_scale", (n_blocks, width, hidden))):
+        a = rng.standard_normal(shape, dtype=np.float32) / np.float32(np.sqrt(shape[-1]))
+        if eight_bit:
+            p[w], p[scale] = _as_i8(a)
+        else:
+            p[w] = f32_to_bf16_bits(a)
+    return p
+
+
 def make_params(cfg, model_seed=1):
     if cfg["kind"] == "gmm":
         return gmm_params(cfg["d"], cfg["C"], cfg["var"], model_seed)
+    if cfg["kind"] == "gated":
+        return gated_params(cfg["d"], cfg["E"], cfg["width"], cfg["hidden"], cfg["n_blocks"], cfg["K"], model_seed,
+                            eight_bit=cfg.get("eight_bit", False), act=cfg.get("act", 0),
+                            predict_eps=cfg.get("predict_eps", False), act_terms=cfg.get("act_terms", 2))
     return mlp_params(cfg["d"], cfg["E"], cfg["width"], cfg["n_blocks"], cfg["K"], model_seed,
                       predict_eps=cfg.get("predict_eps", False), act_terms=cfg.get("act_terms", 2))

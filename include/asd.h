@@ -16,7 +16,7 @@
  *    "DEV" pointers are device (HBM) memory owned by the caller; the library
  *    never frees them.  The denoiser's DEV parameters given to asd_init (GMM:
  *    means, log_w; MLP: biases and the time-embedding table; the MLP weight
- *    matrices are copied) must stay valid until asd_destroy; every other
+ *    matrices are copied; GATED: those of the blocks besides) must stay valid until asd_destroy; every other
  *    pointer is only used by the call it is passed to (asynchronously, on
  *    `stream`).
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).
@@ -72,7 +72,10 @@ typedef struct {
   const int32_t* tau;
 } asd_schedule;
 
-typedef enum { ASD_DEN_GMM = 1, ASD_DEN_MLP = 2 } asd_den_kind;
+typedef enum { ASD_F32 = 0, ASD_BF16 = 1, ASD_F16 = 2, ASD_I8 = 3 } asd_type;
+typedef enum { ASD_ACT_SILU = 0, ASD_ACT_GELU = 1 /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */ } asd_act;
+
+typedef enum { ASD_DEN_GMM = 1, ASD_DEN_MLP = 2, ASD_DEN_GATED = 3 } asd_den_kind;
 
 /* The model g of Alg. 1, as a denoiser D(x, tau) = E[x_0 | x_tau = x].
  *
@@ -105,7 +108,26 @@ typedef enum { ASD_DEN_GMM = 1, ASD_DEN_MLP = 2 } asd_den_kind;
  *   nearest even both times), twice the matrix-core work.  With one term, the rounding of the activations
  *   is amplified by a random-weight residual network to ~2e-3 of its output scale whatever the
  *   accumulation order; with two it is ~4e-6.
- *   linears_per_block must be 1.  d, temb_dim and width must be multiples of 8. */
+ *   linears_per_block must be 1.  d, temb_dim and width must be multiples of 8.
+ * GATED: MLP with gated blocks: n_blocks times
+ *     n = RMSNorm(h) gain_l,  h += W_down_l (act(W_gate_l n) * (W_up_l n));
+ *   everything else as above, and w_blk points to an asd_gated_blocks (HOST; b_blk is not used).  type ASD_BF16: n and the gated
+ *   unit's result are rounded to bf16, the products' sums are fp32.  type ASD_I8: n as 8-bit integers with a scale per row, the
+ *   unit's result to bf16 and from there to 8-bit integers with a scale per row, weights 8-bit integers with a scale per output
+ *   channel (the operators below, on the same numbers).  The blocks' weights are not copied. */
+typedef struct {
+  int32_t hidden;
+  int32_t type, act;    /* ASD_BF16 or ASD_I8; asd_act */
+  double eps;           /* of the norm, >= 0 */
+  const float* gain;    /* DEV fp32 [n_blocks, width], or NULL: 1 */
+  const void* w_gate;   /* DEV [n_blocks, hidden, width] */
+  const void* w_up;
+  const void* w_down;   /* DEV [n_blocks, width, hidden] */
+  const float* gate_scale; /* ASD_I8: DEV fp32 [n_blocks, hidden] */
+  const float* up_scale;
+  const float* down_scale; /* [n_blocks, width] */
+  /* weights on multiples of 16 bytes; width and hidden multiples of 8 (ASD_I8: 16) */
+} asd_gated_blocks;
 typedef struct {
   int32_t kind; /* asd_den_kind */
   int32_t d;
@@ -279,9 +301,6 @@ ASD_API asd_status asd_denoise(asd_ctx* ctx, const float* x, const int32_t* tau,
  *  - rows_used (DEV int32 [1], or NULL): where only the device knows how many of the rows there are.  Rows *rows_used .. rows - 1
  *    of the outputs are left as they were.
  *  - A row's results depend on that row (and the call's sizes) only, and are the same bits every time. */
-typedef enum { ASD_F32 = 0, ASD_BF16 = 1, ASD_F16 = 2, ASD_I8 = 3 } asd_type;
-typedef enum { ASD_ACT_SILU = 0, ASD_ACT_GELU = 1 /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */ } asd_act;
-
 /* asd_rms_norm: r = x + residual (in fp32; residual may be NULL: r = x); sum = r in x's type (NULL: not wanted; may be x or
  *   residual itself, with its pitch); and with rstd = (mean of r^2 + eps)^(-1/2), of r before it is rounded:
  *   out_type ASD_F32, ASD_BF16, ASD_F16: out = r rstd gain.

@@ -152,3 +152,59 @@ class MLPOracle:
         if self.out_clip > 0.0:            # predicted x_0 clipped to the data range
             out = np.clip(out, -self.out_clip, self.out_clip)
         return out
+
+
+def gated_act(z, act):
+    """0: SiLU; 1: the tanh form of GELU."""
+    if act == 0:
+        return silu(z)
+    return 0.5 * z * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (z + 0.044715 * z ** 3)))
+
+
+def rows_to_i8(v):
+    """Rows as integers in -127 .. 127 (ties to even), and their largest magnitudes."""
+    top = np.abs(v).max(axis=1, keepdims=True)
+    return np.where(top > 0, np.rint(127.0 * v / np.where(top > 0, top, 1.0)), 0.0), top
+
+
+class GatedOracle(MLPOracle):
+    """The residual MLP's first and last layer around blocks of n = RMSNorm(h) gain, h += W_down (act(W_gate n) * (W_up n)).
+
+    bf16 blocks: n and the gated unit's result are rounded to bf16.  8-bit blocks: n enters as integers with a scale (fp32) per
+    row, the unit's result is rounded to bf16 and enters the last product in the same way; weights are integers with scales."""
+
+    def __init__(self, params, abar=None):
+        super().__init__(dict(params, w_blk=np.zeros((0, 0, 0), np.uint16), b_blk=np.zeros((0, 0))), abar)
+        self.p = params
+        self.eight_bit = params["block_type"] == 3
+        self.n_blocks = params["w_gate"].shape[0]
+
+    def _weights(self, name, scale, l):
+        if self.eight_bit:
+            return self.p[name][l].astype(np.float64) * self.p[scale][l].astype(np.float64)[:, None]
+        return bf16_bits_to_f64(self.p[name][l])
+
+    def __call__(self, x, tau):
+        x = np.atleast_2d(np.asarray(x, dtype=np.float64))
+        tau = np.broadcast_to(np.asarray(tau, dtype=np.int64), (x.shape[0],))
+        rnd = lambda v: round_to_bf16_terms(v, self.act_terms)      # noqa: E731
+        h = np.concatenate([rnd(x), self.temb[tau]], axis=1) @ self.w_in.T + self.b_in
+        for l in range(self.n_blocks):
+            rstd = 1.0 / np.sqrt((h * h).mean(axis=1, keepdims=True) + self.p["eps"])
+            v = h * self.p["gain"][l].astype(np.float64)
+            if self.eight_bit:
+                q, top = rows_to_i8(v)
+                n = q * (top * rstd / 127.0)
+            else:
+                n = round_to_bf16(v * rstd)
+            u = gated_act(n @ self._weights("w_gate", "gate_scale", l).T, self.p["act"])
+            u = round_to_bf16(u * (n @ self._weights("w_up", "up_scale", l).T))
+            if self.eight_bit:
+                q, top = rows_to_i8(u)
+                u = q * (top / 127.0)
+            h = h + u @ self._weights("w_down", "down_scale", l).T
+        out = rnd(h) @ self.w_out.T + self.b_out
+        if self.predict_eps:
+            ab = self.abar[tau][:, None]
+            out = (x - np.sqrt(1.0 - ab) * out) / np.sqrt(ab)
+        return np.clip(out, -self.out_clip, self.out_clip) if self.out_clip > 0.0 else out

@@ -12,7 +12,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libasd.so")
 
 ASD_OK, ASD_EINVAL, ASD_ENOMEM, ASD_EDEVICE, ASD_ESTATE, ASD_EUNSUPPORTED = 0, -1, -2, -3, -4, -5
-ASD_DEN_GMM, ASD_DEN_MLP = 1, 2
+ASD_DEN_GMM, ASD_DEN_MLP, ASD_DEN_GATED = 1, 2, 3
 ASD_F32, ASD_BF16, ASD_F16, ASD_I8 = 0, 1, 2, 3
 ASD_ACT_SILU, ASD_ACT_GELU = 0, 1
 PROF = dict(MODEL=0, PLAN=1, GMM_ROWWISE=2, GMM_LOGITS=3, GMM_SOFTMAX=4, GMM_COMBINE=5, MLP_PACK=6, MLP_GEMM_IN=7,
@@ -28,6 +28,12 @@ class AsdError(RuntimeError):
 class asd_schedule(C.Structure):
     _fields_ = [("K", C.c_int32), ("c_x", C.c_void_p), ("c_0", C.c_void_p), ("sigma", C.c_void_p),
                 ("tau", C.c_void_p)]
+
+
+class asd_gated_blocks(C.Structure):
+    _fields_ = [("hidden", C.c_int32), ("type", C.c_int32), ("act", C.c_int32), ("eps", C.c_double), ("gain", C.c_void_p),
+                ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p),
+                ("gate_scale", C.c_void_p), ("up_scale", C.c_void_p), ("down_scale", C.c_void_p)]
 
 
 class asd_denoiser(C.Structure):
@@ -244,7 +250,8 @@ def make_config(sched, den, L, chains, seed):
     cfg.sched.c_0 = host(sched["c_0"], np.float32)
     cfg.sched.sigma = host(sched["sigma"], np.float32)
     cfg.sched.tau = host(sched["tau"], np.int32)
-    cfg.den.kind = ASD_DEN_GMM if den["kind"] == "gmm" else ASD_DEN_MLP if den["kind"] == "mlp" else int(den["kind"])
+    kinds = {"gmm": ASD_DEN_GMM, "mlp": ASD_DEN_MLP, "gated": ASD_DEN_GATED}
+    cfg.den.kind = kinds[den["kind"]] if den["kind"] in kinds else int(den["kind"])
     cfg.den.d = int(den["d"])
     cfg.den.n_tau = int(den["n_tau"])
     if den["kind"] == "gmm":
@@ -254,7 +261,7 @@ def make_config(sched, den, L, chains, seed):
         cfg.den.var = float(den["var"])
         cfg.den.abar = host(den["abar"], np.float32) if den.get("abar") is not None else None
         cfg.den.sl_time = host(den["sl_time"], np.float32) if den.get("sl_time") is not None else None
-    elif den["kind"] == "mlp":
+    elif den["kind"] in ("mlp", "gated"):
         cfg.den.width = int(den["width"])
         cfg.den.n_blocks = int(den["n_blocks"])
         cfg.den.linears_per_block = int(den.get("linears_per_block", 1))
@@ -265,6 +272,13 @@ def make_config(sched, den, L, chains, seed):
         cfg.den.abar = host(den["abar"], np.float32) if den.get("abar") is not None else None
         for k in ("w_in", "w_blk", "w_out", "b_in", "b_blk", "b_out", "temb"):
             setattr(cfg.den, k, _ptr(den.get(k)))
+        if den["kind"] == "gated":
+            g = asd_gated_blocks(hidden=int(den["hidden"]), type=int(den.get("block_type", ASD_BF16)),
+                                 act=int(den.get("act", ASD_ACT_SILU)), eps=float(den.get("eps", 1e-6)))
+            for k in ("gain", "w_gate", "w_up", "w_down", "gate_scale", "up_scale", "down_scale"):
+                setattr(g, k, _ptr(den.get(k)))
+            keep.append(g)
+            cfg.den.w_blk = C.addressof(g)
     keep.append(den)
     cfg.L = int(L)
     cfg.chains = int(chains)

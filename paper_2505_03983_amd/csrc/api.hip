@@ -42,6 +42,21 @@ asd_status fail(asd_status s, const char* fmt, ...) {
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // ---- validation (host only; no HIP call) -------------------------------------
+static asd_status validate_blocks(const asd_gated_blocks& b, int32_t width) {
+  if (b.hidden < 1) return fail(ASD_EINVAL, "hidden must be >= 1 (got %d)", b.hidden);
+  if (b.type != ASD_BF16 && b.type != ASD_I8) return fail(ASD_EINVAL, "gated blocks are ASD_BF16 or ASD_I8 (got %d)", b.type);
+  if (b.act != ASD_ACT_SILU && b.act != ASD_ACT_GELU) return fail(ASD_EINVAL, "unknown activation %d", b.act);
+  if (!(b.eps >= 0.0) || !isfinite(b.eps)) return fail(ASD_EINVAL, "eps must be finite and >= 0");
+  if (!b.w_gate || !b.w_up || !b.w_down) return fail(ASD_EINVAL, "gated block weight pointer is NULL");
+  if (!aligned16(b.w_gate) || !aligned16(b.w_up) || !aligned16(b.w_down))
+    return fail(ASD_EINVAL, "gated block weights must be 16-byte aligned");
+  if (b.type == ASD_I8 && (!b.gate_scale || !b.up_scale || !b.down_scale)) return fail(ASD_EINVAL, "8-bit blocks need their scales");
+  const int step = b.type == ASD_I8 ? 16 : 8;
+  if (b.hidden % step || width % step) return fail(ASD_EUNSUPPORTED, "gated blocks need width and hidden to be multiples of %d", step);
+  if (width > 32768 || b.hidden > 32768) return fail(ASD_EUNSUPPORTED, "gated blocks: width and hidden up to 32768");
+  return ASD_OK;
+}
+
 static asd_status validate(const asd_config* cfg) {
   if (!cfg) return fail(ASD_EINVAL, "cfg is NULL");
   const asd_schedule& s = cfg->sched;
@@ -78,7 +93,7 @@ static asd_status validate(const asd_config* cfg) {
     }
     if ((m.d % 4 || m.C % 4) && (int64_t)m.d + m.C > 4096)
       return fail(ASD_EUNSUPPORTED, "GMM denoiser: C=%d, d=%d needs d %% 4 == 0 and C %% 4 == 0 at this size", m.C, m.d);
-  } else if (m.kind == ASD_DEN_MLP) {
+  } else if (m.kind == ASD_DEN_MLP || m.kind == ASD_DEN_GATED) {
     if (m.width < 1 || m.n_blocks < 0 || m.temb_dim < 0) return fail(ASD_EINVAL, "bad MLP shape");
     if (!m.w_in || !m.w_out || (m.n_blocks > 0 && !m.w_blk) || (m.temb_dim > 0 && !m.temb))
       return fail(ASD_EINVAL, "MLP parameter pointer is NULL");
@@ -92,6 +107,7 @@ static asd_status validate(const asd_config* cfg) {
     if (m.linears_per_block != 1) return fail(ASD_EUNSUPPORTED, "linears_per_block must be 1");
     if (m.d % 8 || m.temb_dim % 8 || m.width % 8)
       return fail(ASD_EUNSUPPORTED, "MLP needs d, temb_dim and width to be multiples of 8");
+    if (m.kind == ASD_DEN_GATED && m.n_blocks > 0) ASD_TRY(validate_blocks(*static_cast<const asd_gated_blocks*>(m.w_blk), m.width));
   } else {
     return fail(ASD_EINVAL, "unknown denoiser kind %d", m.kind);
   }
@@ -132,7 +148,7 @@ static asd_status build(asd_ctx* ctx, const asd_config* cfg) {
   ctx->n_tau = cfg->den.n_tau;
   ctx->n_rows_max = (int64_t)cfg->chains * cfg->L;
   ctx->key = make_key(cfg->seed);
-  ctx->kind = cfg->den.kind;
+  ctx->kind = cfg->den.kind == ASD_DEN_GATED ? ASD_DEN_MLP : cfg->den.kind;   // (a network either way: mlp.hip)
   const size_t K = (size_t)ctx->K, rows = (size_t)ctx->n_rows_max;
   ASD_TRY(upload(&ctx->c_x, cfg->sched.c_x, K));
   ASD_TRY(upload(&ctx->c_0, cfg->sched.c_0, K));

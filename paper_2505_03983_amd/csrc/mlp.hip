@@ -15,10 +15,15 @@
 // its output scale, whatever the accumulation order, so two correct implementations of the one-term
 // network differ by that much (0.03-0.05 on outputs clipped to [-1, 1] when the unclipped scale is ~17);
 // with two terms the same figure is ~4e-6 of the output scale.
+//
+// Gated networks (ASD_DEN_GATED): the same first and last layer around blocks of n = RMSNorm(h) gain, h += W_down (act(W_gate n) *
+// (W_up n)), which the operators compute (ops_norm.hip, ops_gemm.hip): the norm adds the last block's result to the fp32 stream h on
+// its way in, and gives n in bf16 or in 8-bit integers with a scale per row.
 #include "common.h"
 #include "gemm_bf16.h"
 #include "gemm_bf16_few.h"
 #include "gemm_bf16_slab.h"
+#include "ops.h"
 
 namespace asd {
 
@@ -174,6 +179,14 @@ struct MlpState {
   uint16_t* hb[2] = {nullptr, nullptr};   // [act_terms][slabs of width][rows_pad][32] each
   int64_t in_plane = 0, h_plane = 0;      // 0 when act_terms == 1
   SplitScratch split;
+  // gated blocks
+  bool gated = false;
+  asd_gated_blocks blocks{};
+  float* delta = nullptr;      // [rows, width]: what a block adds to h
+  void* n = nullptr;           // [rows, width] bf16 or int8
+  uint16_t* u = nullptr;       // [rows, hidden] bf16
+  int8_t* uq = nullptr;        // [rows, hidden], 8-bit blocks
+  float* scales = nullptr;     // [2][rows]: of n's rows, of u's
 };
 
 
@@ -363,6 +376,96 @@ struct SeqEpi {
   }
 };
 
+// hb = bf16 terms of h + delta, in slab layout: what the output layer reads.  Four columns a thread.
+__global__ __launch_bounds__(256) void mlp_stream_kernel(const int* __restrict__ n_dev, int n_rows, int W, const float* __restrict__ h,
+                                                         const float* __restrict__ delta, uint16_t* __restrict__ hb, int64_t slab,
+                                                         int64_t lo_plane) {
+  const int m = blockIdx.x, n = (blockIdx.y * 256 + threadIdx.x) * 4;
+  if (n >= W || m >= min(*n_dev, n_rows)) return;
+  const float4 a = *reinterpret_cast<const float4*>(h + (int64_t)m * W + n), b = *reinterpret_cast<const float4*>(delta + (int64_t)m * W + n);
+  store_act4(hb + (n >> 5) * slab + (int64_t)m * 32 + (n & 31), lo_plane, make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w));
+}
+
+// The blocks of a gated network on h [rows, W]; leaves the last one's result in s->delta.
+static asd_status gated_blocks_eval(MlpState* s, const RowPlan& rows, hipStream_t st) {
+  const asd_gated_blocks& g = s->blocks;
+  const bool i8 = g.type == ASD_I8;
+  const int W = s->width, H = g.hidden, likely = rows.likely;
+  const size_t wb = (size_t)H * W * (i8 ? 1 : 2);
+  float* n_scale = s->scales;
+  for (int l = 0; l < s->n_blocks; ++l) {
+    asd_norm norm{};
+    norm.rows = rows.n;
+    norm.cols = W;
+    norm.type = ASD_F32;
+    norm.out_type = i8 ? ASD_I8 : ASD_BF16;
+    norm.x = s->h;
+    if (l > 0) {
+      norm.residual = s->delta;
+      norm.sum = s->h;
+    }
+    norm.gain = g.gain ? g.gain + (size_t)l * W : nullptr;
+    norm.out = s->n;
+    norm.scale = n_scale;
+    norm.ld_x = norm.ld_residual = norm.ld_sum = norm.ld_out = W;
+    norm.eps = g.eps;
+    norm.rows_used = rows.n_dev;
+    ASD_TRY(launch_rms_norm(norm, st));
+    asd_gated u{};
+    u.rows = rows.n;
+    u.cols = W;
+    u.channels = H;
+    u.type = g.type;
+    u.out_type = ASD_BF16;
+    u.act = g.act;
+    u.x = s->n;
+    u.w_gate = static_cast<const uint8_t*>(g.w_gate) + l * wb;
+    u.w_up = static_cast<const uint8_t*>(g.w_up) + l * wb;
+    if (i8) {
+      u.x_scale = n_scale;
+      u.gate_scale = g.gate_scale + (size_t)l * H;
+      u.up_scale = g.up_scale + (size_t)l * H;
+    }
+    u.out = s->u;
+    u.ld_x = u.ld_w_gate = u.ld_w_up = W;
+    u.ld_out = H;
+    u.rows_used = rows.n_dev;
+    ASD_TRY(launch_gated(u, st, likely));
+    const uint8_t* down = static_cast<const uint8_t*>(g.w_down) + l * wb;
+    if (!i8) {
+      ASD_TRY(launch_linear_bf16(s->u, down, s->delta, rows.n, H, W, rows.n_dev, st, likely));
+      continue;
+    }
+    float* u_scale = s->scales + s->rows_pad;
+    asd_norm q{};
+    q.rows = rows.n;
+    q.cols = H;
+    q.type = ASD_BF16;
+    q.out_type = ASD_I8;
+    q.x = s->u;
+    q.out = s->uq;
+    q.scale = u_scale;
+    q.ld_x = q.ld_out = H;
+    q.rows_used = rows.n_dev;
+    ASD_TRY(launch_quantize_rows(q, st));
+    asd_linear8 d{};
+    d.rows = rows.n;
+    d.cols = H;
+    d.channels = W;
+    d.out_type = ASD_F32;
+    d.x = s->uq;
+    d.x_scale = u_scale;
+    d.w = reinterpret_cast<const int8_t*>(down);
+    d.w_scale = g.down_scale + (size_t)l * W;
+    d.out = s->delta;
+    d.ld_x = d.ld_w = H;
+    d.ld_out = W;
+    d.rows_used = rows.n_dev;
+    ASD_TRY(launch_linear8(d, st, likely));
+  }
+  return ASD_OK;
+}
+
 asd_status mlp_create(asd_ctx* ctx, const asd_denoiser& den) {
   MlpState* s = new (std::nothrow) MlpState();
   if (!s) return ASD_ENOMEM;
@@ -383,14 +486,16 @@ asd_status mlp_create(asd_ctx* ctx, const asd_denoiser& den) {
   }
   s->in_dim = ctx->d + den.temb_dim;
   s->w_in = (const uint16_t*)den.w_in;
-  s->w_blk = (const uint16_t*)den.w_blk;
+  s->gated = den.kind == ASD_DEN_GATED && den.n_blocks > 0;
+  if (s->gated) s->blocks = *static_cast<const asd_gated_blocks*>(den.w_blk);
+  else s->w_blk = (const uint16_t*)den.w_blk;
   s->w_out = (const uint16_t*)den.w_out;
   s->b_in = den.b_in;
   s->b_blk = den.b_blk;
   s->b_out = den.b_out;
   s->temb = (const uint16_t*)den.temb;
   const size_t rows = (size_t)ctx->n_rows_max;
-  ctx->model_macs_per_row = (double)s->in_dim * s->width + (double)s->n_blocks * s->width * s->width +
+  ctx->model_macs_per_row = (double)s->in_dim * s->width + (double)s->n_blocks * s->width * (s->gated ? 3.0 * s->blocks.hidden : s->width) +
                             (double)s->width * ctx->d;
   const int64_t Wd = s->width, dd = ctx->d;
   const size_t planes = (size_t)s->act_terms;
@@ -418,7 +523,15 @@ asd_status mlp_create(asd_ctx* ctx, const asd_denoiser& den) {
   ASD_HIP(hipMalloc(&s->wp_out, sizeof(uint16_t) * slab_elems(dd, s->width)));
   ASD_HIP(pack(s->wp_in, s->w_in, Wd, s->in_dim));
   ASD_HIP(pack(s->wp_out, s->w_out, dd, s->width));
-  if (s->n_blocks) {
+  if (s->gated) {
+    const size_t H = (size_t)s->blocks.hidden;
+    const bool i8 = s->blocks.type == ASD_I8;
+    ASD_HIP(hipMalloc(&s->delta, sizeof(float) * rows * s->width));
+    ASD_HIP(hipMalloc(&s->n, (i8 ? 1 : 2) * rows * s->width));
+    ASD_HIP(hipMalloc(&s->u, sizeof(uint16_t) * rows * H));
+    if (i8) ASD_HIP(hipMalloc(&s->uq, rows * H));
+    ASD_HIP(hipMalloc(&s->scales, sizeof(float) * 2 * (size_t)s->rows_pad));
+  } else if (s->n_blocks) {
     const size_t blk = slab_elems(Wd, s->width);
     ASD_HIP(hipMalloc(&s->wp_blk, sizeof(uint16_t) * s->n_blocks * blk));
     for (int l = 0; l < s->n_blocks; ++l) ASD_HIP(pack(s->wp_blk + l * blk, s->w_blk + (size_t)l * Wd * Wd, Wd, s->width));
@@ -444,6 +557,11 @@ void mlp_destroy(asd_ctx* ctx) {
   (void)hipFree(s->wp_out);
   (void)hipFree(s->eps_coef);
   (void)hipFree(s->split.part);
+  (void)hipFree(s->delta);
+  (void)hipFree(s->n);
+  (void)hipFree(s->u);
+  (void)hipFree(s->uq);
+  (void)hipFree(s->scales);
   delete s;
   ctx->mlp = nullptr;
 }
@@ -456,6 +574,14 @@ PackOut mlp_pack_out(const asd_ctx* ctx) {
 double mlp_call_cost(const asd_ctx* ctx, int call, int rows, int most) {
   const MlpState* s = ctx->mlp;
   const int p = s->act_terms, W = s->width;
+  if (s->gated) {   // (norm, quantiser and the stream's last conversion: a few microseconds each, bound by their rows' bytes)
+    const asd_gated_blocks& g = s->blocks;
+    const bool i8 = g.type == ASD_I8;
+    const int64_t e = i8 ? 1 : 2;
+    const double block = product_us(rows, most, 2 * (int64_t)g.hidden, e * W) + product_us(rows, most, W, e * g.hidden) + 3.0 +
+                         4e-6 * rows * W + (i8 ? 3.0 + 1e-6 * rows * g.hidden : 0.0);
+    return product_cost(p, call, rows, most, W, s->in_dim) + s->n_blocks * block + 3.0 + product_cost(p, call, rows, most, ctx->d, W);
+  }
   return product_cost(p, call, rows, most, W, s->in_dim) + s->n_blocks * product_cost(p, call, rows, most, W, W) +
          product_cost(p, call, rows, most, ctx->d, W);
 }
@@ -467,6 +593,11 @@ uint32_t mlp_verify_tiles(const asd_ctx* ctx, int likely, int most) {
   for (const auto& p : shapes) {   // (as mlp_gemm_planes picks them)
     const int few = pick_few_tile(most, p[0], 1);
     tiles = 8 * tiles + (few >= 0 ? 5 + few : pick_tile(s->act_terms, likely, p[0], slab_count(p[1]) * 32));
+  }
+  if (s->gated) {
+    const asd_gated_blocks& g = s->blocks;
+    const int64_t e = g.type == ASD_I8 ? 1 : 2;
+    tiles = 64 * tiles + 8 * (uint32_t)product_pick(likely, 2 * (int64_t)g.hidden, e * s->width) + (uint32_t)product_pick(likely, s->width, e * g.hidden);
   }
   return tiles;
 }
@@ -493,7 +624,14 @@ asd_status mlp_eval(asd_ctx* ctx, const RowPlan& rows, hipStream_t st) {
   }
   int cur = 0;
   const size_t blk = slab_elems(W, W);
-  for (int l = 0; l < s->n_blocks; ++l) {
+  if (s->gated) {
+    ProfScope ps(ctx, ASD_PROF_MLP_GEMM_BLK, rows.call, st);
+    ASD_TRY(gated_blocks_eval(s, rows, st));
+    hipLaunchKernelGGL(mlp_stream_kernel, dim3((unsigned)n, (unsigned)ceil_div(W, 1024)), dim3(256), 0, st, rows.n_dev, n, W, s->h, s->delta,
+                       s->hb[0], slab, s->h_plane);
+    ASD_HIP(hipGetLastError());
+  }
+  for (int l = 0; !s->gated && l < s->n_blocks; ++l) {
     ProfScope ps(ctx, ASD_PROF_MLP_GEMM_BLK, rows.call, st);
     const BlockEpi e{s->h, s->hb[cur ^ 1], s->b_blk ? s->b_blk + (size_t)l * W : nullptr, W, slab, s->h_plane};
     ASD_HIP(mlp_gemm(rows, W, W, h[cur], SlabMat{s->wp_blk + l * blk, w_rows, 0}, e, st, s->split));

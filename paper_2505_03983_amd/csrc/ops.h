@@ -48,7 +48,15 @@ inline bool on16(const void* p, int64_t ld, int bytes) { return ((uintptr_t)p & 
 // For the library's own launches: the operators without their argument checks.
 asd_status launch_rms_norm(const asd_norm& p, hipStream_t st);
 asd_status launch_quantize_rows(const asd_norm& p, hipStream_t st);
-asd_status launch_linear8(const asd_linear8& p, hipStream_t st);
-asd_status launch_gated(const asd_gated& p, hipStream_t st);
+// likely: rows to expect, where the device knows their number (0: all): which kernel suits, nothing else
+asd_status launch_linear8(const asd_linear8& p, hipStream_t st, int likely = 0);
+asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely = 0);
+// out[m][n] = sum over k of x[m][k] w[n][k]: bf16 rows of whole 16 bytes, side by side, fp32 results
+asd_status launch_linear_bf16(const void* x, const void* w, float* out, int rows, int cols, int channels, const int32_t* rows_used,
+                              hipStream_t st, int likely);
+// Microseconds of a product of `rows` rows with `channels` channels (both matrices' of a gated one) of kb bytes, on the kernel picked
+// for `most` rows; and that kernel's number, below 8.
+double product_us(int rows, int most, int64_t channels, int64_t kb);
+int product_pick(int rows, int64_t channels, int64_t kb);
 
 }  // namespace asd

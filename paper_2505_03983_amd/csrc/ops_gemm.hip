@@ -324,26 +324,23 @@ constexpr int kFewRows = 64;
 constexpr float kFewRate[3] = {4.6f, 2.9f, 1.8f};   // TB/s; up to 16, 32, 64 rows
 
 // 0 .. 2: a tile; 3 .. 5: few rows, 16 .. 64 at a time
+static float kernel_us(int kernel, int M, int64_t n, int64_t kb) {
+  if (kernel >= 3) return 3.f + 1e-6f * (float)n * (float)kb / kFewRate[kernel - 3] * (float)ceil_div(M, 16 << (kernel - 3));
+  const RowsCost& c = kRowsCost[kernel];
+  const int64_t tiles = ceil_div(M, c.bm) * ceil_div(n, c.bn);
+  float rounds = (float)ceil_div(tiles, 256);
+  if (rounds > 2.f) rounds = 0.4f * rounds + 0.6f * (float)tiles / 256.f;
+  return rounds * (tiles > 256 ? c.full : 1.f) * (c.f + c.k * (float)ceil_div(kb, 128));
+}
 static int pick_product(int M, int64_t n, int64_t kb) {
   int best = 0;
-  float least = INFINITY;
-  for (int i = 0; i < 3; ++i) {
-    const RowsCost& c = kRowsCost[i];
-    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(n, c.bn);
-    float rounds = (float)ceil_div(tiles, 256);
-    if (rounds > 2.f) rounds = 0.4f * rounds + 0.6f * (float)tiles / 256.f;
-    const float t = rounds * (tiles > 256 ? c.full : 1.f) * (c.f + c.k * (float)ceil_div(kb, 128));
-    if (t < least) {
-      least = t;
-      best = i;
-    }
-  }
-  if (M <= kFewRows) {
-    const int few = M <= 16 ? 0 : M <= 32 ? 1 : 2;
-    if (3.f + 1e-6f * (float)n * (float)kb / kFewRate[few] < least) best = 3 + few;
-  }
-  return best;
+  for (int i = 1; i < 3; ++i)
+    if (kernel_us(i, M, n, kb) < kernel_us(best, M, n, kb)) best = i;
+  const int few = M <= 16 ? 3 : M <= 32 ? 4 : 5;
+  return M <= kFewRows && kernel_us(few, M, n, kb) < kernel_us(best, M, n, kb) ? few : best;
 }
+int product_pick(int rows, int64_t channels, int64_t kb) { return pick_product(rows, channels, kb); }
+double product_us(int rows, int most, int64_t channels, int64_t kb) { return kernel_us(pick_product(most, channels, kb), rows, channels, kb); }
 
 template <class E, int MT, class Epi>
 static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st) {
@@ -353,8 +350,8 @@ static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st)
 }
 
 template <class E, class Epi>
-static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st) {
-  const int pick = pick_product(p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
+static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st, int likely = 0) {
+  const int pick = pick_product(likely > 0 ? std::min(likely, p.M) : p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
   if constexpr (Epi::kOutputs == 1) {
     if (pick == 3) return launch_few<E, 1>(p, e, st);
     if (pick == 4) return launch_few<E, 2>(p, e, st);
@@ -419,18 +416,29 @@ static Linear8Plan plan_linear8(const asd_linear8& p, void* ws) {
 }
 
 template <class T>
-static asd_status run_linear8(const asd_linear8& p, const Linear8Plan& o, hipStream_t st) {
+static asd_status run_linear8(const asd_linear8& p, const Linear8Plan& o, hipStream_t st, int likely) {
   const RowsProduct g{o.x.p, o.w.p, nullptr, o.x.pitch, o.w.pitch, 0, p.rows, p.channels, k_bytes(p.cols), p.rows_used};
   const Scaled8Epi<T> e{static_cast<T*>(p.out), p.ld_out, p.x_scale, p.w_scale, p.bias, p.channels, on16(p.out, p.ld_out, sizeof(T))};
-  ASD_HIP(launch_product<ElemI8>(g, e, st));
+  ASD_HIP(launch_product<ElemI8>(g, e, st, likely));
   return ASD_OK;
 }
 
-asd_status launch_linear8(const asd_linear8& p, hipStream_t st) {
+asd_status launch_linear8(const asd_linear8& p, hipStream_t st, int likely) {
   const Linear8Plan o = plan_linear8(p, p.workspace);
   ASD_HIP(bring(o.x, st));
   ASD_HIP(bring(o.w, st));
-  return p.out_type == ASD_F32 ? run_linear8<float>(p, o, st) : p.out_type == ASD_BF16 ? run_linear8<__bf16>(p, o, st) : run_linear8<_Float16>(p, o, st);
+  return p.out_type == ASD_F32    ? run_linear8<float>(p, o, st, likely)
+         : p.out_type == ASD_BF16 ? run_linear8<__bf16>(p, o, st, likely)
+                                  : run_linear8<_Float16>(p, o, st, likely);
+}
+
+asd_status launch_linear_bf16(const void* x, const void* w, float* out, int rows, int cols, int channels, const int32_t* rows_used,
+                              hipStream_t st, int likely) {
+  const RowsProduct g{static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(w), nullptr, 2 * (int64_t)cols, 2 * (int64_t)cols, 0, rows,
+                      channels, 2 * (int64_t)cols, rows_used};
+  const SumEpi<float> e{out, nullptr, channels, 0, channels, rows, rows, on16(out, channels, 4)};
+  ASD_HIP(launch_product<ElemBf16>(g, e, st, likely));
+  return ASD_OK;
 }
 
 // ---- the gated unit --------------------------------------------------------------------------------------------------------------
@@ -452,26 +460,26 @@ static RowsProduct gated_product(const asd_gated& p, const GatedPlan& o) {
 }
 
 template <class E, class T>
-static asd_status run_gated(const asd_gated& p, const GatedPlan& o, hipStream_t st) {
+static asd_status run_gated(const asd_gated& p, const GatedPlan& o, hipStream_t st, int likely) {
   const bool wide = on16(p.out, p.ld_out, sizeof(T));
   if constexpr (E::kBytes == 1) {
     const Gated8Epi<T> e{static_cast<T*>(p.out), p.ld_out, p.x_scale, p.gate_scale, p.up_scale, p.channels, p.act, wide};
-    ASD_HIP(launch_product<E>(gated_product(p, o), e, st));
+    ASD_HIP(launch_product<E>(gated_product(p, o), e, st, likely));
   } else {
     const GatedEpi<T> e{static_cast<T*>(p.out), p.ld_out, p.channels, p.act, wide};
-    ASD_HIP(launch_product<E>(gated_product(p, o), e, st));
+    ASD_HIP(launch_product<E>(gated_product(p, o), e, st, likely));
   }
   return ASD_OK;
 }
 
-asd_status launch_gated(const asd_gated& p, hipStream_t st) {
+asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely) {
   Carve c{static_cast<uint8_t*>(p.workspace)};
   const GatedPlan o = plan_gated(p, &c);
   ASD_HIP(bring(o.x, st));
   ASD_HIP(bring(o.g, st));
   ASD_HIP(bring(o.u, st));
-  if (p.type == ASD_I8) return p.out_type == ASD_BF16 ? run_gated<ElemI8, __bf16>(p, o, st) : run_gated<ElemI8, _Float16>(p, o, st);
-  return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st) : run_gated<ElemF16, _Float16>(p, o, st);
+  if (p.type == ASD_I8) return p.out_type == ASD_BF16 ? run_gated<ElemI8, __bf16>(p, o, st, likely) : run_gated<ElemI8, _Float16>(p, o, st, likely);
+  return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st, likely) : run_gated<ElemF16, _Float16>(p, o, st, likely);
 }
 
 // Gradient.  g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract

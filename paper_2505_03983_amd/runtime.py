@@ -23,8 +23,14 @@ def device_params(cfg, params, device="cuda:0"):
     out = dict(kind="mlp", d=cfg["d"], width=cfg["width"], n_blocks=cfg["n_blocks"], temb_dim=cfg["E"],
                out_clip=float(params.get("out_clip", 0.0)), predict_eps=bool(params.get("predict_eps", False)),
                act_terms=int(params.get("act_terms", 1)))
+    if cfg["kind"] == "gated":
+        out.update(kind="gated", hidden=cfg["hidden"], **{k: params[k] for k in ("block_type", "act", "eps") if k in params})
+        for k in ("gain", "w_gate", "w_up", "w_down", "gate_scale", "up_scale", "down_scale"):
+            if k in params:
+                out[k] = up(params[k])
     for k in ("w_in", "w_blk", "w_out", "b_in", "b_blk", "b_out", "temb"):
-        out[k] = up(params[k])
+        if k in params:
+            out[k] = up(params[k])
     return out
 
 

@@ -132,3 +132,19 @@ def test_gated_gradient_workspace():
     assert L.asd_gated_ff_backward_workspace(None) == 0 and L.asd_gated_ff_workspace(None) == 0
     assert w() > w(dx=None) > 0 and w() > w(dw_gate=None, dw_up=None) > 0 and w(rows=0) == 0
     assert L.asd_gated_ff(C.byref(gated(rows=0, x=None)), None) == b.ASD_OK
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(hidden=0), EINVAL), (dict(block_type=b.ASD_F32), EINVAL), (dict(act=5), EINVAL), (dict(eps=-1.0), EINVAL),
+    (dict(w_up=None), EINVAL), (dict(w_down=24), EINVAL), (dict(hidden=20), EUNSUPPORTED), (dict(hidden=65536), EUNSUPPORTED),
+    (dict(block_type=b.ASD_I8), EINVAL), (dict(block_type=b.ASD_I8, gate_scale=16, up_scale=16, down_scale=16, width=24), EUNSUPPORTED),
+    (dict(w_out=None), EINVAL), (dict(d=12), EUNSUPPORTED),
+])
+def test_gated_network_refusals(kw, status):
+    s = b.asd_schedule_ddpm_linear(10)
+    den = dict(kind="gated", d=16, n_tau=11, width=32, hidden=48, n_blocks=2, temb_dim=8, w_in=16, w_out=16, temb=16, w_gate=16, w_up=16,
+               w_down=16)
+    den.update(kw)
+    with pytest.raises(b.AsdError) as e:
+        b.Ctx(s, den, 4, 2)
+    assert e.value.status == status, b.last_error()
