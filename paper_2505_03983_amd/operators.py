@@ -26,10 +26,12 @@ def _matrix(t, name, dtype, device, rows, cols):
     """Address and row pitch of a matrix argument."""
     if t.shape != (rows, cols):
         _refuse("%s has shape %s, not %s" % (name, tuple(t.shape), (rows, cols)))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
+    if t.is_contiguous():
+        return t.data_ptr(), cols
     row, col = t.stride()
     if col != 1 and cols > 1:
         _refuse("the columns of %s do not lie next to each other" % name)
@@ -45,18 +47,28 @@ def _vector(t, name, dtype, device, n):
         return None
     if t.shape != (n,):
         _refuse("%s has shape %s, not (%d,)" % (name, tuple(t.shape), n))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
-    if n > 1 and t.stride(0) != 1:
+    if not t.is_contiguous():
         _refuse("the elements of %s do not lie next to each other" % name)
     return t.data_ptr()
 
 
-def _new(out, shape, dtype, device):
-    """An output argument, or a new array."""
-    return torch.empty(shape, dtype=dtype, device=device) if out is None else out
+def _out(t, name, dtype, device, rows, cols):
+    """An output matrix, a new one if none is given: the tensor, its address and row pitch."""
+    if t is None:
+        t = torch.empty((rows, cols), dtype=dtype, device=device)
+        return t, t.data_ptr(), cols
+    return (t, *_matrix(t, name, dtype, device, rows, cols))
+
+
+def _out_vector(t, name, dtype, device, n):
+    if t is None:
+        t = torch.empty(n, dtype=dtype, device=device)
+        return t, t.data_ptr()
+    return t, _vector(t, name, dtype, device, n)
 
 
 def _rows_of(x, name="x"):
@@ -103,18 +115,16 @@ def rms_norm(x, gain=None, eps=1e-6, residual=None, out_type=None, out=None, sca
         _refuse("no such type: %s -> %s" % (t, out_type))
     a = binding.asd_norm(rows=rows, cols=cols, type=_TYPE[t], out_type=_TYPE[out_type], eps=eps)
     a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
-    out = _new(out, (rows, cols), out_type, dev)
-    a.out, a.ld_out = _matrix(out, "out", out_type, dev, rows, cols)
+    out, a.out, a.ld_out = _out(out, "out", out_type, dev, rows, cols)
     a.gain = _vector(gain, "gain", t, dev, cols)
     if residual is not None:
         a.residual, a.ld_residual = _matrix(residual, "residual", t, dev, rows, cols)
         if sum_out is None:
-            sum_out = torch.empty((rows, cols), dtype=t, device=dev)
-    if sum_out is not None:
+            sum_out, a.sum, a.ld_sum = _out(None, "sum_out", t, dev, rows, cols)
+    if sum_out is not None and not a.sum:
         a.sum, a.ld_sum = _matrix(sum_out, "sum_out", t, dev, rows, cols)
     if out_type == torch.int8:
-        scale = _new(scale, (rows,), torch.float32, dev)
-        a.scale = _vector(scale, "scale", torch.float32, dev, rows)
+        scale, a.scale = _out_vector(scale, "scale", torch.float32, dev, rows)
     else:
         scale = None
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
@@ -130,10 +140,8 @@ def quantize_rows(x, out=None, scale=None, rows_used=None, stream=None):
         _refuse("no such type: %s" % t)
     a = binding.asd_norm(rows=rows, cols=cols, type=_TYPE[t], out_type=binding.ASD_I8)
     a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
-    out = _new(out, (rows, cols), torch.int8, dev)
-    a.out, a.ld_out = _matrix(out, "out", torch.int8, dev, rows, cols)
-    scale = _new(scale, (rows,), torch.float32, dev)
-    a.scale = _vector(scale, "scale", torch.float32, dev, rows)
+    out, a.out, a.ld_out = _out(out, "out", torch.int8, dev, rows, cols)
+    scale, a.scale = _out_vector(scale, "scale", torch.float32, dev, rows)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
     _launch("asd_quantize_rows", a, dev, stream, workspace=False)
     return out, scale
@@ -152,10 +160,8 @@ def rms_norm_backward(dy, total, gain=None, eps=1e-6, dsum=None, dx=None, dgain=
     if dsum is not None:
         a.dsum, a.ld_dsum = _matrix(dsum, "dsum", t, dev, rows, cols)
     a.gain = _vector(gain, "gain", t, dev, cols)
-    dx = _new(dx, (rows, cols), t, dev)
-    a.dx, a.ld_dx = _matrix(dx, "dx", t, dev, rows, cols)
-    dgain = _new(dgain, (cols,), t, dev)
-    a.dgain = _vector(dgain, "dgain", t, dev, cols)
+    dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, rows, cols)
+    dgain, a.dgain = _out_vector(dgain, "dgain", t, dev, cols)
     _launch("asd_rms_norm_backward", a, dev, stream)
     return dx, dgain
 
@@ -173,8 +179,7 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, out_type=torch.bfloat16, out=No
     a.x_scale = _vector(x_scale, "x_scale", torch.float32, dev, rows)
     a.w_scale = _vector(w_scale, "w_scale", torch.float32, dev, channels)
     a.bias = _vector(bias, "bias", torch.float32, dev, channels)
-    out = _new(out, (rows, channels), out_type, dev)
-    a.out, a.ld_out = _matrix(out, "out", out_type, dev, rows, channels)
+    out, a.out, a.ld_out = _out(out, "out", out_type, dev, rows, channels)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
     _launch("asd_linear_i8", a, dev, stream)
     return out
@@ -206,8 +211,7 @@ def gated_ff(x, w_gate, w_up, act="silu", x_scale=None, gate_scale=None, up_scal
         a.x_scale = _vector(x_scale, "x_scale", torch.float32, dev, a.rows)
         a.gate_scale = _vector(gate_scale, "gate_scale", torch.float32, dev, a.channels)
         a.up_scale = _vector(up_scale, "up_scale", torch.float32, dev, a.channels)
-    out = _new(out, (a.rows, a.channels), out_type, dev)
-    a.out, a.ld_out = _matrix(out, "out", out_type, dev, a.rows, a.channels)
+    out, a.out, a.ld_out = _out(out, "out", out_type, dev, a.rows, a.channels)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
     _launch("asd_gated_ff", a, dev, stream)
     return out
@@ -220,15 +224,12 @@ def gated_ff_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=Tru
     dev, t = x.device, x.dtype
     a.dh, a.ld_dh = _matrix(dh, "dh", t, dev, a.rows, a.channels)
     if need_dx:
-        dx = _new(dx, (a.rows, a.cols), t, dev)
-        a.dx, a.ld_dx = _matrix(dx, "dx", t, dev, a.rows, a.cols)
+        dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, a.rows, a.cols)
     else:
         dx = None
     if need_dw:
-        dw_gate = _new(dw_gate, (a.channels, a.cols), t, dev)
-        dw_up = _new(dw_up, (a.channels, a.cols), t, dev)
-        a.dw_gate, a.ld_dw_gate = _matrix(dw_gate, "dw_gate", t, dev, a.channels, a.cols)
-        a.dw_up, a.ld_dw_up = _matrix(dw_up, "dw_up", t, dev, a.channels, a.cols)
+        dw_gate, a.dw_gate, a.ld_dw_gate = _out(dw_gate, "dw_gate", t, dev, a.channels, a.cols)
+        dw_up, a.dw_up, a.ld_dw_up = _out(dw_up, "dw_up", t, dev, a.channels, a.cols)
     else:
         dw_gate = dw_up = None
     _launch("asd_gated_ff_backward", a, dev, stream)

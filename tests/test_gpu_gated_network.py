@@ -92,7 +92,9 @@ def test_sequential_and_windows_of_one(eight_bit):
 
 @pytest.mark.parametrize("control", [False, True])
 def test_windows_in_pieces_and_by_the_controller(control):
-    """Sizes at which windows are taken in pieces or rounds differ in rows."""
+    """Sizes at which windows are taken in pieces or rounds differ in rows.  A random-weight network is no contraction: over 60 steps
+    the 2e-3 that two correct model calls differ by grows to a tenth of the state.  So every round is compared from the device's own
+    state, where a round's rows hold one model call's difference, scaled by c_0 < 1."""
     cfg = dict(kind="gated", d=112, E=128, width=512, hidden=1376, n_blocks=3, K=60, chains=64, L=16, eight_bit=True)
     T, p, model, runtime = setup(cfg)
     ctx = runtime.open_ctx(cfg, p, seed=7)
@@ -104,6 +106,6 @@ def test_windows_in_pieces_and_by_the_controller(control):
         assert bool(torch.isfinite(a).all())
         assert 60 / 16 <= float(rounds.min()) and float(rounds.max()) <= 60
         for c in (5, 60):
-            f = H.follow_chain(cfg, T, model, 7, c, a[c].cpu().numpy(), 2e-2, adaptive=control)
-            assert H.rel_err(a[c].cpu().numpy(), f["y"]) <= 2e-2
+            f = H.follow_chain(cfg, T, model, 7, c, a[c].cpu().numpy(), 2e-2, adaptive=control, resync=True)
+            assert f["a"] == 60 and f["R"] == int(rounds[c]) and f["round_err"] <= 2e-2, f["round_err"]
     ctx.close()
