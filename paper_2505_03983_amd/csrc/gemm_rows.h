@@ -133,8 +133,8 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / Cfg::WGN, wn = wave % Cfg::WGN;
   const int lrow = lane % B, part = lane / B;
   typedef typename Epi::Out Out;
-  constexpr int COLS = Cfg::WN / (GATED ? 2 : 1), OB = (int)sizeof(Out);
-  constexpr int ROWB = COLS * OB, SL = ROWB / 16;           // bytes and slots of a row
+  constexpr int COLS = Cfg::WN / (GATED ? 2 : 1), OB = (int)sizeof(Out), OUTS = Epi::kOutputs;
+  constexpr int ROWB = OUTS * COLS * OB, SL = ROWB / 16;    // bytes and slots of a parked row: one output after the other
   static_assert(NW * B * ROWB <= Cfg::PIPE_BYTES, "parked results");
   static_assert(SL >= 2 && SL <= 64 && (SL & (SL - 1)) == 0, "slots of a parked row");
   constexpr int FACTOR = GATED ? 32 / B : 0;                // blocks from a gate's to the matching up's
@@ -148,49 +148,62 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
 #pragma unroll
     for (int q = 0; q < RUNS; ++q)
       if (!(GATED && (j * B / 32) % 2)) cc[j][q] = epi.cols(col0 + column(j, q));
-  for (int out = 0; out < Epi::kOutputs; ++out) {
+  // what a result takes besides (dh, in a gradient) is fetched a block of rows ahead
+  typename Epi::Extra extra[2][NB][RUNS];
+  auto fetch = [&](int i) {
+    const int m = min(m0 + wm * Cfg::WM + i * B + lrow, M - 1);
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      const int mrow = m0 + wm * Cfg::WM + i * B;
-      if (mrow >= M) break;
-      const int m = min(mrow + lrow, M - 1);
-      const auto rc = epi.row(m);
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        if (GATED && (j * B / 32) % 2) continue;
+      for (int q = 0; q < RUNS; ++q)
+        if (!(GATED && (j * B / 32) % 2)) extra[i & 1][j][q] = epi.extra(m, col0 + column(j, q));
+  };
+  fetch(0);
 #pragma unroll
-        for (int q = 0; q < RUNS; ++q) {
-          const int c = column(j, q);
-          typename E::Sum a[4], b[4];
+  for (int i = 0; i < MB; ++i) {
+    const int mrow = m0 + wm * Cfg::WM + i * B;
+    if (mrow >= M) break;
+    if (i + 1 < MB) fetch(i + 1);
+    const int m = min(mrow + lrow, M - 1);
+    const auto rc = epi.row(m);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            a[r] = acc[j][i][4 * q + r];
-            b[r] = acc[j + FACTOR][i][4 * q + r];
-          }
-          Out v[4];
-          epi.values(out, rc, cc[j][q], m, col0 + c, a, b, v);
-          const int byte = c * OB, sl = (byte >> 4) ^ (lrow & (SL - 1));
-          if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + lrow * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v);
-          else *reinterpret_cast<uint4*>(park + lrow * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v);
+    for (int j = 0; j < NB; ++j) {
+      if (GATED && (j * B / 32) % 2) continue;
+#pragma unroll
+      for (int q = 0; q < RUNS; ++q) {
+        const int c = column(j, q);
+        typename E::Sum a[4], b[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          a[r] = acc[j][i][4 * q + r];
+          b[r] = acc[j + FACTOR][i][4 * q + r];
+        }
+        Out v[OUTS][4];
+        epi.values(rc, cc[j][q], extra[i & 1][j][q], col0 + c, a, b, v);
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o) {
+          const int byte = (o * COLS + c) * OB, sl = (byte >> 4) ^ (lrow & (SL - 1));
+          if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + lrow * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v[o]);
+          else *reinterpret_cast<uint4*>(park + lrow * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v[o]);
         }
       }
-      // (the region is this wavefront's own, whose LDS operations complete in order)
-      if (!epi.wide) {   // rows at no multiple of 16 bytes: number by number, neighbours by neighbouring lanes
+    }
+    // (the region is this wavefront's own, whose LDS operations complete in order)
+    if (!epi.wide) {   // rows at no multiple of 16 bytes: number by number, neighbours by neighbouring lanes
 #pragma unroll 4
-        for (int e = lane; e < B * COLS; e += 64) {
-          const int r = e / COLS, byte = e % COLS * OB;
-          const Out v = *reinterpret_cast<const Out*>(park + r * ROWB + (((byte >> 4) ^ (r & (SL - 1))) * 16) + (byte & 15));
-          if (mrow + r < M) epi.store1(mrow + r, col0 + e % COLS, v);
-        }
-        continue;
+      for (int e = lane; e < B * COLS; e += 64) {
+        const int r = e / COLS, byte = e % COLS * OB;
+        const Out v = *reinterpret_cast<const Out*>(park + r * ROWB + (((byte >> 4) ^ (r & (SL - 1))) * 16) + (byte & 15));
+        if (mrow + r < M) epi.store1(mrow + r, col0 + e % COLS, v);
       }
-      constexpr int RPI = 64 / SL < B ? 64 / SL : B;        // rows a pass of the wavefront covers
+      continue;
+    }
+    constexpr int RPI = 64 / SL < B ? 64 / SL : B;        // rows a pass of the wavefront covers
 #pragma unroll
-      for (int r0 = 0; r0 < B; r0 += RPI) {
-        const int r = r0 + lane / SL, sl = lane % SL;
-        const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
-        if (lane < RPI * SL && mrow + r < M) epi.store(out, mrow + r, col0 + sl * (16 / OB), v);
-      }
+    for (int r0 = 0; r0 < B; r0 += RPI) {
+      const int r = r0 + lane / SL, sl = lane % SL;
+      const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
+      if (lane < RPI * SL && mrow + r < M) epi.store(sl / (SL / OUTS), mrow + r, col0 + sl % (SL / OUTS) * (16 / OB), v);
     }
   }
 }

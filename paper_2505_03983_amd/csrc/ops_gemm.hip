@@ -41,9 +41,11 @@ struct SumEpi {
   __device__ __forceinline__ Row row(int) const { return Row{}; }
   struct Cols {};
   __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
-  __device__ __forceinline__ void values(int, Row, Cols, int, int, const float* a, const float*, T* v) const {
+  struct Extra {};
+  __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
+  __device__ __forceinline__ void values(Row, Cols, Extra, int, const float* a, const float*, T (&v)[1][4]) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (T)a[r];
+    for (int r = 0; r < 4; ++r) v[0][r] = (T)a[r];
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const {
     if (m < first_rows) store_cols(out + m * ld, n, N, v);
@@ -76,6 +78,8 @@ struct Scaled8Epi {
   struct Cols {
     float s[4], b[4];
   };
+  struct Extra {};
+  __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
   __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
   __device__ __forceinline__ Cols cols(int n) const {
     Cols c;
@@ -86,9 +90,9 @@ struct Scaled8Epi {
     }
     return c;
   }
-  __device__ __forceinline__ void values(int, float xs, const Cols& c, int, int, const int* a, const int*, T* v) const {
+  __device__ __forceinline__ void values(float xs, const Cols& c, Extra, int, const int* a, const int*, T (&v)[1][4]) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (T)((float)a[r] * xs * c.s[r] + c.b[r]);
+    for (int r = 0; r < 4; ++r) v[0][r] = (T)((float)a[r] * xs * c.s[r] + c.b[r]);
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
   __device__ __forceinline__ void store1(int m, int n, T v) const {
@@ -129,9 +133,11 @@ struct GatedEpi {
   __device__ __forceinline__ Row row(int) const { return Row{}; }
   struct Cols {};
   __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
-  __device__ __forceinline__ void values(int, Row, Cols, int, int, const float* g, const float* u, T* v) const {
+  struct Extra {};
+  __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
+  __device__ __forceinline__ void values(Row, Cols, Extra, int, const float* g, const float* u, T (&v)[1][4]) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (T)(act_value(act, g[r]) * u[r]);
+    for (int r = 0; r < 4; ++r) v[0][r] = (T)(act_value(act, g[r]) * u[r]);
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
   __device__ __forceinline__ void store1(int m, int n, T v) const {
@@ -155,6 +161,8 @@ struct Gated8Epi {
   struct Cols {
     float g[4], u[4];
   };
+  struct Extra {};
+  __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
   __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
   __device__ __forceinline__ Cols cols(int n) const {
     Cols c;
@@ -168,9 +176,9 @@ struct Gated8Epi {
   __device__ __forceinline__ T value(float xs, float gs, float us, int g, int u) const {
     return (T)(act_value(act, (float)g * xs * gs) * ((float)u * xs * us));
   }
-  __device__ __forceinline__ void values(int, float xs, const Cols& c, int, int, const int* g, const int* u, T* v) const {
+  __device__ __forceinline__ void values(float xs, const Cols& c, Extra, int, const int* g, const int* u, T (&v)[1][4]) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = value(xs, c.g[r], c.u[r], g[r], u[r]);
+    for (int r = 0; r < 4; ++r) v[0][r] = value(xs, c.g[r], c.u[r], g[r], u[r]);
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
   __device__ __forceinline__ void store1(int m, int n, T v) const {
@@ -196,21 +204,28 @@ struct GatedGradEpi {
   __device__ __forceinline__ Row row(int) const { return Row{}; }
   struct Cols {};
   __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
-  __device__ __forceinline__ void values(int which, Row, Cols, int m, int n, const float* g, const float* u, T* v) const {
-    T dv[4];
+  struct Extra {
+    T dh[4];
+  };
+  __device__ __forceinline__ Extra extra(int m, int n) const {
+    Extra x;
     const T* at = dh + m * ld_dh + n;
     if (dh_wide && n + 4 <= N) {
-      *reinterpret_cast<uint2*>(dv) = *reinterpret_cast<const uint2*>(at);
+      *reinterpret_cast<uint2*>(x.dh) = *reinterpret_cast<const uint2*>(at);
     } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) dv[r] = n + r < N ? at[r] : (T)0.f;
+      for (int r = 0; r < 4; ++r) x.dh[r] = n + r < N ? at[r] : (T)0.f;
     }
+    return x;
+  }
+  __device__ __forceinline__ void values(Row, Cols, const Extra& x, int n, const float* g, const float* u, T (&v)[2][4]) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float d = (float)dv[r];
+      const float d = (float)x.dh[r];
       float value, slope;
       act_both(act, g[r], &value, &slope);
-      v[r] = n + r < N ? (T)(which ? d * value : d * u[r] * slope) : (T)0.f;
+      v[0][r] = n + r < N ? (T)(d * u[r] * slope) : (T)0.f;
+      v[1][r] = n + r < N ? (T)(d * value) : (T)0.f;
     }
   }
   static constexpr bool wide = true;
