@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "gemm_rows.h"
 #include "ops.h"
@@ -236,29 +237,43 @@ struct GatedGradEpi {
 };
 
 // ---- passes over operands --------------------------------------------------------------------------------------------------
-// Rows of `bytes` bytes at any address and pitch, copied to rows on multiples of 128 bytes, zeros behind them.  Sixteen bytes of
-// the copy a thread.
-__global__ __launch_bounds__(256) void pack_rows_kernel(const uint8_t* __restrict__ src, int64_t pitch, int rows, int64_t bytes,
-                                                        uint8_t* __restrict__ dst, int64_t dst_pitch) {
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16;
-  const int64_t row = at / dst_pitch, k = at - row * dst_pitch;
-  if (row >= rows) return;
-  const uint8_t* s = src + row * pitch + k;
+// Rows of `bytes` bytes at any address and pitch, copied to rows on multiples of 128 bytes, zeros behind them.
+struct RowsCopy {
+  const uint8_t* src;
+  uint8_t* dst;
+  int64_t pitch, dst_pitch, bytes;
+  int rows;
+  int64_t chunks() const { return dst_pitch / 16 * rows; }
+};
+struct RowsCopies {
+  RowsCopy c[3];
+  unsigned first[3];   // its first workgroup
+  int n;
+};
+// Sixteen bytes of a copy a thread.
+__global__ __launch_bounds__(256) void pack_rows_kernel(RowsCopies all) {
+  int i = 0;
+  while (i + 1 < all.n && blockIdx.x >= all.first[i + 1]) ++i;
+  const RowsCopy& c = all.c[i];
+  const int64_t at = ((int64_t)(blockIdx.x - all.first[i]) * 256 + threadIdx.x) * 16;
+  const int64_t row = at / c.dst_pitch, k = at - row * c.dst_pitch;
+  if (row >= c.rows) return;
+  const uint8_t* s = c.src + row * c.pitch + k;
   uint32_t v[4] = {0u, 0u, 0u, 0u};
-  if (k > 0 && k + 20 <= bytes) {   // five words around the sixteen bytes, all of this row
+  if (k > 0 && k + 20 <= c.bytes) {   // five words around the sixteen bytes, all of this row
     const int shift = (int)((uintptr_t)s & 3);
     const uint32_t* w = reinterpret_cast<const uint32_t*>(s - shift);
     uint32_t a[5];
 #pragma unroll
-    for (int i = 0; i < 5; ++i) a[i] = w[i];
+    for (int j = 0; j < 5; ++j) a[j] = w[j];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(a[i + 1], a[i], shift);
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbyte(a[j + 1], a[j], shift);
   } else {
 #pragma unroll
     for (int b = 0; b < 16; ++b)
-      if (k + b < bytes) v[b >> 2] |= (uint32_t)s[b] << (8 * (b & 3));
+      if (k + b < c.bytes) v[b >> 2] |= (uint32_t)s[b] << (8 * (b & 3));
   }
-  *reinterpret_cast<uint4*>(dst + at) = make_uint4(v[0], v[1], v[2], v[3]);
+  *reinterpret_cast<uint4*>(c.dst + at) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
@@ -393,24 +408,29 @@ struct Carve {
 struct Operand {
   const uint8_t* p;
   int64_t pitch;   // bytes
-  uint8_t* copy;   // NULL: none
-  const uint8_t* src;
-  int64_t src_pitch;
-  int rows;
-  int64_t bytes;
+  bool copied;
+  RowsCopy copy;
 };
 static Operand operand(const void* p, int rows, int64_t cols, int64_t ld, int bytes, Carve* ws) {
   const int64_t row = cols * bytes;
+  const uint8_t* src = static_cast<const uint8_t*>(p);
   if (on16(p, rows > 1 ? ld : 0, bytes) && (row & 15) == 0 && (rows == 1 || ld * bytes <= kMaxPitch))
-    return Operand{static_cast<const uint8_t*>(p), rows > 1 ? ld * bytes : row, nullptr, nullptr, 0, rows, row};
+    return Operand{src, rows > 1 ? ld * bytes : row, false, RowsCopy{}};
   const int64_t pitch = ceil_div(row, 128) * 128;
   uint8_t* c = ws->take((size_t)pitch * rows);
-  return Operand{c, pitch, c ? c : reinterpret_cast<uint8_t*>(1), static_cast<const uint8_t*>(p), ld * bytes, rows, row};
+  return Operand{c, pitch, true, RowsCopy{src, c, ld * bytes, pitch, row, rows}};
 }
-static hipError_t bring(const Operand& o, hipStream_t st) {
-  if (!o.copy) return hipSuccess;
-  const int64_t threads = o.pitch / 16 * o.rows;
-  hipLaunchKernelGGL(pack_rows_kernel, dim3((unsigned)ceil_div(threads, 256)), dim3(256), 0, st, o.src, o.src_pitch, o.rows, o.bytes, o.copy, o.pitch);
+static hipError_t bring(std::initializer_list<const Operand*> operands, hipStream_t st) {
+  RowsCopies all{};
+  int64_t grid = 0;
+  for (const Operand* o : operands) {
+    if (!o->copied) continue;
+    all.first[all.n] = (unsigned)grid;
+    all.c[all.n++] = o->copy;
+    grid += ceil_div(o->copy.chunks(), 256);
+  }
+  if (!all.n) return hipSuccess;
+  hipLaunchKernelGGL(pack_rows_kernel, dim3((unsigned)grid), dim3(256), 0, st, all);
   return hipGetLastError();
 }
 // Bytes of k the kernels run over: copies have zeros behind their rows.
@@ -440,8 +460,7 @@ static asd_status run_linear8(const asd_linear8& p, const Linear8Plan& o, hipStr
 
 asd_status launch_linear8(const asd_linear8& p, hipStream_t st, int likely) {
   const Linear8Plan o = plan_linear8(p, p.workspace);
-  ASD_HIP(bring(o.x, st));
-  ASD_HIP(bring(o.w, st));
+  ASD_HIP(bring({&o.x, &o.w}, st));
   return p.out_type == ASD_F32    ? run_linear8<float>(p, o, st, likely)
          : p.out_type == ASD_BF16 ? run_linear8<__bf16>(p, o, st, likely)
                                   : run_linear8<_Float16>(p, o, st, likely);
@@ -490,9 +509,7 @@ static asd_status run_gated(const asd_gated& p, const GatedPlan& o, hipStream_t 
 asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely) {
   Carve c{static_cast<uint8_t*>(p.workspace)};
   const GatedPlan o = plan_gated(p, &c);
-  ASD_HIP(bring(o.x, st));
-  ASD_HIP(bring(o.g, st));
-  ASD_HIP(bring(o.u, st));
+  ASD_HIP(bring({&o.x, &o.g, &o.u}, st));
   if (p.type == ASD_I8) return p.out_type == ASD_BF16 ? run_gated<ElemI8, __bf16>(p, o, st, likely) : run_gated<ElemI8, _Float16>(p, o, st, likely);
   return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st, likely) : run_gated<ElemF16, _Float16>(p, o, st, likely);
 }
@@ -536,9 +553,7 @@ __global__ __launch_bounds__(256) void zero16_kernel(uint16_t* p, int64_t ld, in
 template <class E, class T>
 static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   const GatedGradPlan o = plan_gated_grad(p);
-  ASD_HIP(bring(o.in.x, st));
-  ASD_HIP(bring(o.in.g, st));
-  ASD_HIP(bring(o.in.u, st));
+  ASD_HIP(bring({&o.in.x, &o.in.g, &o.in.u}, st));
   T* dgu = reinterpret_cast<T*>(o.dgu);
   const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act,
                           ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0};

@@ -14,6 +14,8 @@
 // 16 bytes.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ops.h"
 
 namespace asd {
@@ -104,9 +106,13 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
   const T* x = static_cast<const T*>(p.x) + row * p.ld_x;
   const T* res = NORM && p.residual ? static_cast<const T*>(p.residual) + row * p.ld_residual : nullptr;
   const T* gain = NORM ? static_cast<const T*>(p.gain) : nullptr;
-  float r[RUNS][kRun];
+  // (the quantiser's rows stay in their own type: half the registers, twice the rows in flight)
+  Run<typename std::conditional<NORM, float, T>::type> r[RUNS];
   Run<T> g[RUNS];
-  {
+  if constexpr (!NORM) {
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) fetch_run<WIDE>(x, p.cols, THREADS, t, c, r[c]);
+  } else {
     Run<T> a[RUNS], b[RUNS];
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) fetch_run<WIDE>(x, p.cols, THREADS, t, c, a[c]);
@@ -123,7 +129,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
 #pragma unroll
     for (int c = 0; c < RUNS; ++c)
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) r[c][k] = res ? (float)a[c].v[k] + (float)b[c].v[k] : (float)a[c].v[k];
+      for (int k = 0; k < kRun; ++k) r[c].v[k] = res ? (float)a[c].v[k] + (float)b[c].v[k] : (float)a[c].v[k];
   }
   if (NORM && p.sum) {
     T* sum = static_cast<T*>(p.sum) + row * p.ld_sum;
@@ -131,24 +137,33 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
     for (int c = 0; c < RUNS; ++c) {
       Run<T> v;
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) v.v[k] = (T)r[c][k];
+      for (int k = 0; k < kRun; ++k) v.v[k] = (T)r[c].v[k];
       store_run<WIDE>(sum, p.cols, THREADS, t, c, v);
     }
   }
   // odd: NaN as soon as one of the row's v is not a number below infinity
   double squares = 0.0, odd = 0.0, top = 0.0;
+  float odd32 = 0.f, top32 = 0.f;
 #pragma unroll
   for (int c = 0; c < RUNS; ++c)
 #pragma unroll
     for (int k = 0; k < kRun; ++k) {
-      const double d = (double)r[c][k];
+      const double d = (double)(float)r[c].v[k];
       if constexpr (NORM) squares = fma(d, d, squares);
-      if constexpr (I8) {
-        const double v = NORM ? d * (double)(float)g[c].v[k] : d;
+      if constexpr (I8 && NORM) {
+        const double v = d * (double)(float)g[c].v[k];
         odd = fma(v, 0.0, odd);
         top = fmax(top, fabs(v));
       }
+      if constexpr (I8 && !NORM) {
+        odd32 = fmaf((float)r[c].v[k], 0.f, odd32);
+        top32 = fmaxf(top32, fabsf((float)r[c].v[k]));
+      }
     }
+  if constexpr (I8 && !NORM) {
+    odd = (double)odd32;
+    top = (double)top32;
+  }
   row_total<THREADS>(squares, odd, top, lds);
   const double rstd = NORM ? 1.0 / sqrt(squares / (double)p.cols + p.eps) : 1.0;
   O* out = static_cast<O*>(p.out) + row * p.ld_out;
@@ -157,15 +172,30 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
     const double inv = 1.0 / top;
     if (t == 0) p.scale[row] = !good ? __uint_as_float(0x7fc00000u) : top > 0.0 ? (float)(top * rstd / 127.0) : 0.f;
     const bool some = good && top > 0.0;
+    // (127 / top may leave fp32, and so may v: such rows, of numbers next to either end of fp32's range, are done exactly throughout)
+    const bool plain = top > 1e-30 && top < 1e30;
+    const float fast = (float)(127.0 * inv);
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) {
+      // In fp32 first: the quotient is off by less than 127 times a few 2^-24, 1e-4 with room to spare, so an integer is wrong
+      // only if the quotient seems that near to a border; a run that holds such a number (one in eighty) is done exactly.
       Run<int8_t> q;
+      float nearest = 0.f;
 #pragma unroll
       for (int k = 0; k < kRun; ++k) {
-        const double d = (double)r[c][k], a = 127.0 * (NORM ? d * (double)(float)g[c].v[k] : d);
-        const double q0 = a * inv, q1 = fma(fma(-q0, top, a), inv, q0);
-        q.v[k] = some ? (int8_t)(int)rint(q1) : (int8_t)0;
+        const float z = (NORM ? (float)r[c].v[k] * (float)g[c].v[k] : (float)r[c].v[k]) * fast, n = rintf(z);
+        nearest = fmaxf(nearest, fabsf(z - n));
+        q.v[k] = (int8_t)(int)n;
       }
+      if (!plain || nearest > 0.4999f) {
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+          const double d = (double)(float)r[c].v[k], a = 127.0 * (NORM ? d * (double)(float)g[c].v[k] : d);
+          const double q0 = a * inv, q1 = fma(fma(-q0, top, a), inv, q0);
+          q.v[k] = (int8_t)(int)rint(q1);
+        }
+      }
+      if (!some) q = Run<int8_t>{};
       store_run<WIDE>(out, p.cols, THREADS, t, c, q);
     }
   } else {
@@ -173,7 +203,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
     for (int c = 0; c < RUNS; ++c) {
       Run<O> v;
 #pragma unroll
-      for (int k = 0; k < kRun; ++k) v.v[k] = (O)((float)((double)r[c][k] * rstd) * (float)g[c].v[k]);   // (rstd alone may leave fp32)
+      for (int k = 0; k < kRun; ++k) v.v[k] = (O)((float)((double)(float)r[c].v[k] * rstd) * (float)g[c].v[k]);   // (rstd alone may leave fp32)
       store_run<WIDE>(out, p.cols, THREADS, t, c, v);
     }
   }
@@ -290,7 +320,8 @@ __global__ __launch_bounds__(1024) void norm_gain_grad_kernel(int cols, int n_pa
 // f(threads, runs) as constants for rows of `cols`: a wavefront a row up to 1024 numbers, four up to 6144, sixteen from there.  Few
 // runs a thread leave registers for more rows in flight: 16384 rows of 8192 bf16 numbers with a residual into integers 257 us with
 // four runs in four wavefronts, 233 with one in sixteen.
-template <class F>
+// The quantiser (LEAN), whose rows take half the registers: four wavefronts up to 16384.
+template <bool LEAN, class F>
 static asd_status by_width(int cols, F f) {
   typedef std::integral_constant<int, 64> W1;
   typedef std::integral_constant<int, 256> W4;
@@ -300,6 +331,11 @@ static asd_status by_width(int cols, F f) {
   if (runs(64) <= 2) return f(W1(), std::integral_constant<int, 2>());
   if (runs(256) <= 1) return f(W4(), std::integral_constant<int, 1>());
   if (runs(256) <= 2) return f(W4(), std::integral_constant<int, 2>());
+  if constexpr (LEAN) {
+    if (runs(256) <= 4) return f(W4(), std::integral_constant<int, 4>());
+    if (runs(256) <= 8) return f(W4(), std::integral_constant<int, 8>());
+    return f(W16(), std::integral_constant<int, 4>());
+  }
   if (runs(256) <= 3) return f(W4(), std::integral_constant<int, 3>());
   if (runs(1024) <= 1) return f(W16(), std::integral_constant<int, 1>());
   if (runs(1024) <= 2) return f(W16(), std::integral_constant<int, 2>());
@@ -314,7 +350,7 @@ static asd_status run_norm(const asd_norm& p, hipStream_t st) {
   if (NORM)
     wide = wide && (!p.residual || on16(p.residual, p.ld_residual, sizeof(T))) && (!p.sum || on16(p.sum, p.ld_sum, sizeof(T))) &&
            ((uintptr_t)p.gain & 15) == 0;
-  return by_width(p.cols, [&](auto threads, auto runs) -> asd_status {
+  return by_width<!NORM && sizeof(T) == 2>(p.cols, [&](auto threads, auto runs) -> asd_status {
     constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
     const dim3 grid((unsigned)ceil_div(p.rows, PER)), block(TH * PER);
     if (wide) hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM, true>), grid, block, 0, st, p);
@@ -384,7 +420,7 @@ static asd_status run_norm_grad(const asd_norm_grad& p, hipStream_t st) {
              (!p.dsum || on16(p.dsum, p.ld_dsum, sizeof(T))) && (!p.dx || on16(p.dx, p.ld_dx, sizeof(T)));
   float* parts = p.dgain ? static_cast<float*>(p.workspace) : nullptr;
   if (p.rows > 0) {
-    ASD_TRY(by_width(p.cols, [&](auto threads, auto runs) -> asd_status {
+    ASD_TRY(by_width<false>(p.cols, [&](auto threads, auto runs) -> asd_status {
       constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
       const dim3 grid((unsigned)norm_grad_wgs(p.rows, p.cols)), block(TH * PER);
       if (wide) hipLaunchKernelGGL((rms_norm_grad_kernel<T, TH, R, true>), grid, block, 0, st, p, parts);
