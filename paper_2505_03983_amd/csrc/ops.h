@@ -45,6 +45,13 @@ inline asd_status check_mats(const MatArg* m, int n) {
 // Rows at any 16 bytes: what the wide loads and stores ask for.
 inline bool on16(const void* p, int64_t ld, int bytes) { return ((uintptr_t)p & 15) == 0 && (ld * bytes & 15) == 0; }
 
+// n workgroups as a grid (a dimension times its threads stays below 2^32), and a workgroup's number in it.
+inline dim3 grid_of(int64_t n) {
+  const int64_t x = n < 65536 ? n : 65536;
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+__device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // For the library's own launches: the operators without their argument checks.
 asd_status launch_rms_norm(const asd_norm& p, hipStream_t st);
 asd_status launch_quantize_rows(const asd_norm& p, hipStream_t st);

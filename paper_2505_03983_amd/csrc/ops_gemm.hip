@@ -243,37 +243,40 @@ struct RowsCopy {
   uint8_t* dst;
   int64_t pitch, dst_pitch, bytes;
   int rows;
-  int64_t chunks() const { return dst_pitch / 16 * rows; }
 };
 struct RowsCopies {
   RowsCopy c[3];
-  unsigned first[3];   // its first workgroup
+  int64_t first[3];   // its first workgroup
   int n;
 };
-// Sixteen bytes of a copy a thread.
-__global__ __launch_bounds__(256) void pack_rows_kernel(RowsCopies all) {
+// A row a wavefront, sixteen bytes of the copy a thread at a time.
+constexpr int kCopyRows = 4;   // rows a workgroup
+__global__ __launch_bounds__(64 * kCopyRows) void pack_rows_kernel(RowsCopies all) {
   int i = 0;
-  while (i + 1 < all.n && blockIdx.x >= all.first[i + 1]) ++i;
+  while (i + 1 < all.n && workgroup() >= all.first[i + 1]) ++i;
   const RowsCopy& c = all.c[i];
-  const int64_t at = ((int64_t)(blockIdx.x - all.first[i]) * 256 + threadIdx.x) * 16;
-  const int64_t row = at / c.dst_pitch, k = at - row * c.dst_pitch;
+  const int64_t row = (workgroup() - all.first[i]) * kCopyRows + (threadIdx.x >> 6);
   if (row >= c.rows) return;
-  const uint8_t* s = c.src + row * c.pitch + k;
-  uint32_t v[4] = {0u, 0u, 0u, 0u};
-  if (k > 0 && k + 20 <= c.bytes) {   // five words around the sixteen bytes, all of this row
-    const int shift = (int)((uintptr_t)s & 3);
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(s - shift);
-    uint32_t a[5];
+  const uint8_t* src = c.src + row * c.pitch;
+  uint8_t* dst = c.dst + row * c.dst_pitch;
+  const int shift = (int)((uintptr_t)src & 3);
+#pragma unroll 2
+  for (int64_t k = (threadIdx.x & 63) * 16; k < c.dst_pitch; k += 1024) {
+    uint32_t v[4] = {0u, 0u, 0u, 0u};
+    if (k > 0 && k + 20 <= c.bytes) {   // five words around the sixteen bytes, all of this row
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(src + k - shift);
+      uint32_t a[5];
 #pragma unroll
-    for (int j = 0; j < 5; ++j) a[j] = w[j];
+      for (int j = 0; j < 5; ++j) a[j] = w[j];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbyte(a[j + 1], a[j], shift);
-  } else {
+      for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbyte(a[j + 1], a[j], shift);
+    } else {
 #pragma unroll
-    for (int b = 0; b < 16; ++b)
-      if (k + b < c.bytes) v[b >> 2] |= (uint32_t)s[b] << (8 * (b & 3));
+      for (int b = 0; b < 16; ++b)
+        if (k + b < c.bytes) v[b >> 2] |= (uint32_t)src[k + b] << (8 * (b & 3));
+    }
+    *reinterpret_cast<uint4*>(dst + k) = make_uint4(v[0], v[1], v[2], v[3]);
   }
-  *reinterpret_cast<uint4*>(c.dst + at) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
@@ -381,7 +384,8 @@ static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st)
 
 template <class E, class Epi>
 static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st, int likely = 0) {
-  const int pick = pick_product(likely > 0 ? std::min(likely, p.M) : p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
+  int pick = pick_product(likely > 0 ? std::min(likely, p.M) : p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
+  if (pick >= 3 && ceil_div(p.M, 16 << (pick - 3)) > 65535) pick = 2;   // (few are likely of very many: a dimension of the grid)
   if constexpr (Epi::kOutputs == 1) {
     if (pick == 3) return launch_few<E, 1>(p, e, st);
     if (pick == 4) return launch_few<E, 2>(p, e, st);
@@ -425,12 +429,12 @@ static hipError_t bring(std::initializer_list<const Operand*> operands, hipStrea
   int64_t grid = 0;
   for (const Operand* o : operands) {
     if (!o->copied) continue;
-    all.first[all.n] = (unsigned)grid;
+    all.first[all.n] = grid;
     all.c[all.n++] = o->copy;
-    grid += ceil_div(o->copy.chunks(), 256);
+    grid += ceil_div(o->copy.rows, kCopyRows);
   }
   if (!all.n) return hipSuccess;
-  hipLaunchKernelGGL(pack_rows_kernel, dim3((unsigned)grid), dim3(256), 0, st, all);
+  hipLaunchKernelGGL(pack_rows_kernel, grid_of(grid), dim3(64 * kCopyRows), 0, st, all);
   return hipGetLastError();
 }
 // Bytes of k the kernels run over: copies have zeros behind their rows.
@@ -546,7 +550,7 @@ static hipError_t transpose16(const void* src, int64_t ld, int rows, int cols, u
 }
 
 __global__ __launch_bounds__(256) void zero16_kernel(uint16_t* p, int64_t ld, int rows, int cols) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t at = workgroup() * 256 + threadIdx.x;
   if (at < (int64_t)rows * cols) p[at / cols * ld + at % cols] = 0;
 }
 
@@ -692,12 +696,13 @@ asd_status asd_gated_ff_backward(const asd_gated* p, void* stream) {
   if (p->rows == 0) {
     const int64_t n = (int64_t)p->channels * p->cols;
     if (p->dw_gate) {
-      hipLaunchKernelGGL(zero16_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, static_cast<uint16_t*>(p->dw_gate), p->ld_dw_gate, p->channels, p->cols);
-      hipLaunchKernelGGL(zero16_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, static_cast<uint16_t*>(p->dw_up), p->ld_dw_up, p->channels, p->cols);
+      hipLaunchKernelGGL(zero16_kernel, grid_of(ceil_div(n, 256)), dim3(256), 0, st, static_cast<uint16_t*>(p->dw_gate), p->ld_dw_gate, p->channels, p->cols);
+      hipLaunchKernelGGL(zero16_kernel, grid_of(ceil_div(n, 256)), dim3(256), 0, st, static_cast<uint16_t*>(p->dw_up), p->ld_dw_up, p->channels, p->cols);
       ASD_HIP(hipGetLastError());
     }
     return ASD_OK;
   }
+  if (!p->dx && !p->dw_gate) return ASD_OK;
   return p->type == ASD_BF16 ? run_gated_grad<ElemBf16, __bf16>(*p, st) : run_gated_grad<ElemF16, _Float16>(*p, st);
 }
 

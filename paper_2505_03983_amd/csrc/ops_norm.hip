@@ -101,7 +101,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
   __shared__ double lds[THREADS / 64][3];
   const int rows = p.rows_used ? min(max(*p.rows_used, 0), p.rows) : p.rows;
   const int t = threadIdx.x % THREADS;
-  const int row = (int)blockIdx.x * PER_WG + (PER_WG > 1 ? (int)threadIdx.x / THREADS : 0);
+  const int64_t row = workgroup() * PER_WG + (PER_WG > 1 ? (int)threadIdx.x / THREADS : 0);
   if (row >= rows) return;   // (whole workgroups, or wavefronts that wait for nobody)
   const T* x = static_cast<const T*>(p.x) + row * p.ld_x;
   const T* res = NORM && p.residual ? static_cast<const T*>(p.residual) + row * p.ld_residual : nullptr;
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_grad_k
   const int part = (int)blockIdx.x * PER_WG + lane_row, n_parts = (int)gridDim.x * PER_WG;
   Run<T> g[RUNS], r[RUNS], dy[RUNS];
   Run<float> dg[RUNS];
-  auto fetch = [&](int row) {
+  auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < RUNS; ++c) {
       fetch_run<WIDE>(static_cast<const T*>(p.sum) + row * p.ld_sum, p.cols, THREADS, t, c, r[c]);
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_grad_k
     }
   }
   int turn = 0;
-  for (int row = part; row < p.rows; row += n_parts) {
+  for (int64_t row = part; row < p.rows; row += n_parts) {
     Run<T> rn[RUNS], dyn[RUNS], ds[RUNS];
     if (!AHEAD) fetch(row);
 #pragma unroll
@@ -352,7 +352,7 @@ static asd_status run_norm(const asd_norm& p, hipStream_t st) {
            ((uintptr_t)p.gain & 15) == 0;
   return by_width<!NORM && sizeof(T) == 2>(p.cols, [&](auto threads, auto runs) -> asd_status {
     constexpr int TH = decltype(threads)::value, R = decltype(runs)::value, PER = TH < 256 ? 256 / TH : 1;
-    const dim3 grid((unsigned)ceil_div(p.rows, PER)), block(TH * PER);
+    const dim3 grid = grid_of(ceil_div(p.rows, PER)), block(TH * PER);
     if (wide) hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM, true>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((rms_norm_kernel<T, O, TH, R, NORM, false>), grid, block, 0, st, p);
     ASD_HIP(hipGetLastError());

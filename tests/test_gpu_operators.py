@@ -496,6 +496,48 @@ def test_offsets_past_32_bits():
     assert float(x[-1, -1]) == 32.0 and float(x[-1, :-1].abs().max()) == 0 and float(x[: rows - 1].abs().max()) == 0
 
 
+def test_more_rows_than_threads_in_a_dimension():
+    """70 million rows of 8, four to a workgroup: 2^32 threads and more."""
+    o = O()
+    rows = 70_000_000
+    x = torch.ones(rows, 8, dtype=F16, device=DEV)
+    x[-1] = 2.0
+    q, s = o.quantize_rows(x)
+    assert bool((q == 127).all()) and float(s[0]) == float(s[rows // 2]) and float(s[-1]) == 2 * float(s[0])
+    y, _, _ = o.rms_norm(x, eps=0.0)
+    assert bool((y == 1.0).all())
+    dx, dgain = o.rms_norm_backward(y, x, eps=0.0)
+    assert float(dx.float().abs().max()) == 0.0 and dgain.shape == (8,)
+
+
+def test_first_call_in_a_graph():
+    """Kernels that no call has used before, captured at once (in a process of its own: nothing is warm there)."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2505_03983_amd import operators as O
+x = torch.randn(600, 512, device="cuda:0").half()
+w = torch.randn(8192, 512, device="cuda:0").half() / 20
+g = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(g):
+    h = O.gated_ff(x, w, w, "gelu")
+    dx, dg, du = O.gated_ff_backward(h, x, w, w, "gelu")
+g.replay()
+torch.cuda.synchronize()
+want = O.gated_ff(x, w, w, "gelu")
+assert torch.equal(h, want)
+a = O.gated_ff_backward(want, x, w, w, "gelu")
+assert torch.equal(dx, a[0]) and torch.equal(dg, a[1]) and torch.equal(du, a[2])
+print("done")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=100)
+    assert r.stdout.strip().endswith("done"), r.stderr[-2000:]
+
+
 def test_refused_tensors():
     o = O()
     x, w = torch.zeros(4, 32, dtype=BF16, device=DEV), torch.zeros(8, 32, dtype=BF16, device=DEV)
