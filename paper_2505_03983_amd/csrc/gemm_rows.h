@@ -274,6 +274,7 @@ __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[j][i][r] = 0;
 
+  uint4 part[LPS];   // the partial stage, on its way (it is parked when the loads behind it are)
   if (rest) {
 #pragma unroll
     for (int q = 0; q < LPS; ++q) {
@@ -281,9 +282,8 @@ __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, 
       const int at = (slot ^ key_of(b * RPL + sub_row)) * 16;
       const uint8_t* base = q < X_LOADS ? p.x + (int64_t)m0 * p.x_pitch
                             : second(q - X_LOADS) ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0;
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (at < rest) v = *reinterpret_cast<const uint4*>(base + (q < X_LOADS ? x_off[q < X_LOADS ? q : 0] : w_off[q < X_LOADS ? 0 : q - X_LOADS]));
-      *reinterpret_cast<uint4*>(rows_lds + (q < X_LOADS ? 0 : BM * BKB) + b * 1024 + lane * 16) = v;
+      part[q] = make_uint4(0u, 0u, 0u, 0u);
+      if (at < rest) part[q] = *reinterpret_cast<const uint4*>(base + (q < X_LOADS ? x_off[q < X_LOADS ? q : 0] : w_off[q < X_LOADS ? 0 : q - X_LOADS]));
     }
   } else if (nk > 0) {
     issue(0, rows_lds, 0, LPS);
@@ -291,6 +291,11 @@ __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, 
 #pragma unroll
   for (int s = 1; s < STAGES - 1; ++s)
     if (s < nk) issue(s, rows_lds + s * Cfg::STAGE_BYTES, 0, LPS);
+  if (rest) {
+#pragma unroll
+    for (int q = 0; q < LPS; ++q)
+      *reinterpret_cast<uint4*>(rows_lds + (q < X_LOADS ? (wave + NW * q) * 1024 : BM * BKB + (wave + NW * (q - X_LOADS)) * 1024) + lane * 16) = part[q];
+  }
 
   v4i_b xf[2][MI], wf[2][NJ];
   const int x_row = (wm * Cfg::WM + l32) * BKB, w_row = BM * BKB + (wn * Cfg::WN + l32) * BKB;
@@ -463,17 +468,17 @@ __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int t
   };
 
   // the first stage, through registers if it is what is left of k over whole stages (zeros behind it), and the second
+  uint4 part[2][2][2];   // (parked when the loads behind it are on their way)
   if (rest) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const int xk = (slot ^ (((x_blk[h][q] * 8 + sub) >> 1) & 7)) * 16, wk = (slot ^ (((w_blk[h][q] * 8 + sub) >> 1) & 7)) * 16;
-        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-        if (xk < rest) a = *reinterpret_cast<const uint4*>(p.x + (int64_t)m0 * p.x_pitch + x_off[h][q]);
-        if (wk < rest) b = *reinterpret_cast<const uint4*>((GATED && h ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0) + w_off[h][q]);
-        *reinterpret_cast<uint4*>(rows_lds + x_blk[h][q] * 1024 + lane * 16) = a;
-        *reinterpret_cast<uint4*>(rows_lds + w_blk[h][q] * 1024 + lane * 16) = b;
+        part[h][q][0] = part[h][q][1] = make_uint4(0u, 0u, 0u, 0u);
+        if (xk < rest) part[h][q][0] = *reinterpret_cast<const uint4*>(p.x + (int64_t)m0 * p.x_pitch + x_off[h][q]);
+        if (wk < rest)
+          part[h][q][1] = *reinterpret_cast<const uint4*>((GATED && h ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0) + w_off[h][q]);
       }
   } else {
     issue(0, 0);
@@ -482,10 +487,18 @@ __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int t
   if (nk > 1) {
     issue(1, 0);
     issue(1, 1);
-    wait_vmcnt<8>();
-  } else {
-    wait_vmcnt<0>();
   }
+  if (rest) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        *reinterpret_cast<uint4*>(rows_lds + x_blk[h][q] * 1024 + lane * 16) = part[h][q][0];
+        *reinterpret_cast<uint4*>(rows_lds + w_blk[h][q] * 1024 + lane * 16) = part[h][q][1];
+      }
+  }
+  if (nk > 1) wait_vmcnt<8>();
+  else wait_vmcnt<0>();
   lds_handover();
   read_x(0, 0);
   read_w(0, 0);

@@ -259,24 +259,21 @@ __global__ __launch_bounds__(64 * kCopyRows) void pack_rows_kernel(RowsCopies al
   if (row >= c.rows) return;
   const uint8_t* src = c.src + row * c.pitch;
   uint8_t* dst = c.dst + row * c.dst_pitch;
-  const int shift = (int)((uintptr_t)src & 3);
-#pragma unroll 2
-  for (int64_t k = (threadIdx.x & 63) * 16; k < c.dst_pitch; k += 1024) {
-    uint32_t v[4] = {0u, 0u, 0u, 0u};
-    if (k > 0 && k + 20 <= c.bytes) {   // five words around the sixteen bytes, all of this row
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(src + k - shift);
-      uint32_t a[5];
+  const int lane = threadIdx.x & 63, shift = (int)((uintptr_t)src & 3);
+  // inside the row: five words around the sixteen bytes, all of this row; the first sixteen and the end byte by byte
+  const int64_t inner = c.bytes < 36 ? 16 : (c.bytes - 20) / 16 * 16 + 16;
+#pragma unroll 4
+  for (int64_t k = 16 + lane * 16; k < inner; k += 1024) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(src + k - shift);
+    uint32_t a[5], v[4];
 #pragma unroll
-      for (int j = 0; j < 5; ++j) a[j] = w[j];
+    for (int j = 0; j < 5; ++j) a[j] = w[j];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbyte(a[j + 1], a[j], shift);
-    } else {
-#pragma unroll
-      for (int b = 0; b < 16; ++b)
-        if (k + b < c.bytes) v[b >> 2] |= (uint32_t)src[k + b] << (8 * (b & 3));
-    }
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbyte(a[j + 1], a[j], shift);
     *reinterpret_cast<uint4*>(dst + k) = make_uint4(v[0], v[1], v[2], v[3]);
   }
+  if (lane < 16) dst[lane] = lane < c.bytes ? src[lane] : (uint8_t)0;
+  for (int64_t k = inner + lane; k < c.dst_pitch; k += 64) dst[k] = k < c.bytes ? src[k] : (uint8_t)0;
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next

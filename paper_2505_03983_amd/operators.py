@@ -56,10 +56,14 @@ def _vector(t, name, dtype, device, n):
     return t.data_ptr()
 
 
-def _out(t, name, dtype, device, rows, cols):
-    """An output matrix, a new one if none is given: the tensor, its address and row pitch."""
+def _out(t, name, dtype, device, rows, cols, like=None):
+    """An output matrix, a new one if none is given (like: a matrix of its shape; quicker): the tensor, its address and row
+    pitch."""
     if t is None:
-        t = torch.empty((rows, cols), dtype=dtype, device=device)
+        if like is not None and like.is_contiguous():
+            t = torch.empty_like(like, dtype=dtype)
+        else:
+            t = torch.empty((rows, cols), dtype=dtype, device=device)
         return t, t.data_ptr(), cols
     return (t, *_matrix(t, name, dtype, device, rows, cols))
 
@@ -115,12 +119,12 @@ def rms_norm(x, gain=None, eps=1e-6, residual=None, out_type=None, out=None, sca
         _refuse("no such type: %s -> %s" % (t, out_type))
     a = binding.asd_norm(rows=rows, cols=cols, type=_TYPE[t], out_type=_TYPE[out_type], eps=eps)
     a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
-    out, a.out, a.ld_out = _out(out, "out", out_type, dev, rows, cols)
+    out, a.out, a.ld_out = _out(out, "out", out_type, dev, rows, cols, x)
     a.gain = _vector(gain, "gain", t, dev, cols)
     if residual is not None:
         a.residual, a.ld_residual = _matrix(residual, "residual", t, dev, rows, cols)
         if sum_out is None:
-            sum_out, a.sum, a.ld_sum = _out(None, "sum_out", t, dev, rows, cols)
+            sum_out, a.sum, a.ld_sum = _out(None, "sum_out", t, dev, rows, cols, x)
     if sum_out is not None and not a.sum:
         a.sum, a.ld_sum = _matrix(sum_out, "sum_out", t, dev, rows, cols)
     if out_type == torch.int8:
@@ -140,7 +144,7 @@ def quantize_rows(x, out=None, scale=None, rows_used=None, stream=None):
         _refuse("no such type: %s" % t)
     a = binding.asd_norm(rows=rows, cols=cols, type=_TYPE[t], out_type=binding.ASD_I8)
     a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
-    out, a.out, a.ld_out = _out(out, "out", torch.int8, dev, rows, cols)
+    out, a.out, a.ld_out = _out(out, "out", torch.int8, dev, rows, cols, x)
     scale, a.scale = _out_vector(scale, "scale", torch.float32, dev, rows)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
     _launch("asd_quantize_rows", a, dev, stream, workspace=False)
@@ -160,7 +164,7 @@ def rms_norm_backward(dy, total, gain=None, eps=1e-6, dsum=None, dx=None, dgain=
     if dsum is not None:
         a.dsum, a.ld_dsum = _matrix(dsum, "dsum", t, dev, rows, cols)
     a.gain = _vector(gain, "gain", t, dev, cols)
-    dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, rows, cols)
+    dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, rows, cols, total)
     dgain, a.dgain = _out_vector(dgain, "dgain", t, dev, cols)
     _launch("asd_rms_norm_backward", a, dev, stream)
     return dx, dgain
@@ -224,7 +228,7 @@ def gated_ff_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=Tru
     dev, t = x.device, x.dtype
     a.dh, a.ld_dh = _matrix(dh, "dh", t, dev, a.rows, a.channels)
     if need_dx:
-        dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, a.rows, a.cols)
+        dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, a.rows, a.cols, x)
     else:
         dx = None
     if need_dw:
