@@ -297,7 +297,8 @@ ASD_API asd_status asd_denoise(asd_ctx* ctx, const float* x, const int32_t* tau,
  *  - `workspace` (16-byte aligned, workspace_bytes long; what it holds before does not matter) is the caller's, and one call's
  *    until that call's work on the stream is over: calls on different streams, or graphs that may run at the same time, need
  *    their own.  asd_*_workspace(args) says how many bytes a call with these sizes, types, pitches and pointers needs; 0: none,
- *    workspace may be NULL.  (Forward products need one only where rows start at no multiple of 16 bytes.)
+ *    workspace may be NULL.  (Forward products need one
+ *    where rows start at no multiple of 16 bytes, and 8-bit ones with few results of long sums, which are added in parts.)
  *  - rows_used (DEV int32 [1], or NULL): where only the device knows how many of the rows there are.  Rows *rows_used .. rows - 1
  *    of the outputs are left as they were.
  *  - A row's results depend on that row (and the call's sizes) only, and are the same bits every time. */

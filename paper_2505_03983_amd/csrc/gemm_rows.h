@@ -208,9 +208,21 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
   }
 }
 
+// The share of k of a launch that splits it (gridDim.y workgroups a tile): whole stages, the last one takes what is left.
+__device__ __forceinline__ void take_share(RowsProduct& p) {
+  const int64_t share = (p.kb + 128 * (int64_t)gridDim.y - 1) / (128 * (int64_t)gridDim.y) * 128, from = min(share * blockIdx.y, p.kb);
+  p.x += from;
+  p.w0 += from;
+  p.kb = min(share, p.kb - from);
+}
+
 template <class E, class Cfg, class Epi>
 __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
   constexpr bool GATED = Epi::kGated;
+  if constexpr (Epi::kSplit) {
+    take_share(p);
+    epi.out += blockIdx.y * epi.part_stride;
+  }
   constexpr int BM = Cfg::BM, BN = Cfg::BN, MI = Cfg::MI, NJ = Cfg::NJ, BKB = Cfg::BKB, STAGES = Cfg::STAGES, NG = Cfg::NG;
   constexpr int X_LOADS = Cfg::X_LOADS, W_LOADS = Cfg::W_LOADS, LPS = Cfg::LPS, NW = Cfg::NW, RPL = Cfg::RPL;
   constexpr int CPR = BKB / 16;                       // chunks of 16 bytes per row of a stage
@@ -386,6 +398,10 @@ template <class E, class Epi>
 __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
   typedef Rows256 Cfg;
   constexpr bool GATED = Epi::kGated;
+  if constexpr (Epi::kSplit) {
+    take_share(p);
+    epi.out += blockIdx.y * epi.part_stride;
+  }
   constexpr int BM = 256, BKB = 128;
   extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
 
@@ -480,7 +496,7 @@ __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int t
         if (wk < rest)
           part[h][q][1] = *reinterpret_cast<const uint4*>((GATED && h ? p.w1 + (int64_t)n0 * p.w_pitch1 : p.w0 + (int64_t)n0 * p.w_pitch0) + w_off[h][q]);
       }
-  } else {
+  } else if (nk > 0) {   // (a share of k may be empty)
     issue(0, 0);
     issue(0, 1);
   }
@@ -555,9 +571,14 @@ __global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi e
   const uint8_t* wrow[WT];
   wrow[0] = p.w0 + (int64_t)min(n0 + l16, p.N - 1) * p.w_pitch0;
   if constexpr (GATED) wrow[1] = p.w1 + (int64_t)min(n0 + l16, p.N - 1) * p.w_pitch1;
+  // (lanes of rows that are not there load nothing: with one row, a sixteenth of the requests)
   const uint8_t* xrow[MT];
+  bool there[MT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xrow[i] = p.x + (int64_t)min(m0 + i * 16 + l16, M - 1) * p.x_pitch;
+  for (int i = 0; i < MT; ++i) {
+    there[i] = m0 + i * 16 + l16 < M;
+    xrow[i] = p.x + (int64_t)min(m0 + i * 16 + l16, M - 1) * p.x_pitch;
+  }
   typename E::Acc16 acc[WT][MT];
 #pragma unroll
   for (int t = 0; t < WT; ++t)
@@ -577,7 +598,7 @@ __global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi e
 #pragma unroll
         for (int t = 0; t < WT; ++t) wf[s][h][t] = in ? __builtin_nontemporal_load(reinterpret_cast<const v4i_b*>(wrow[t] + k)) : zero;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xf[s][h][i] = in ? *reinterpret_cast<const v4i_b*>(xrow[i] + k) : zero;
+        for (int i = 0; i < MT; ++i) xf[s][h][i] = in && there[i] ? *reinterpret_cast<const v4i_b*>(xrow[i] + k) : zero;
       }
 #pragma unroll
     for (int s = 0; s < DEPTH; ++s)
@@ -597,7 +618,7 @@ __global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi e
   __syncthreads();
   for (int e = tid; e < MT * 256; e += 512) {
     const int i = e >> 8, row = (e >> 4) & 15, c = e & 15, m = m0 + i * 16 + row, n = n0 + c;
-    if (m >= M || n >= p.N) continue;
+    if (m >= M || n >= epi.columns()) continue;
     typename E::Sum a = part[0][0][i][row][c], b = part[0][WT - 1][i][row][c];
 #pragma unroll
     for (int w = 1; w < NWAVES; ++w) {

@@ -461,7 +461,7 @@ static asd_status gated_blocks_eval(MlpState* s, const RowPlan& rows, hipStream_
     d.ld_x = d.ld_w = H;
     d.ld_out = W;
     d.rows_used = rows.n_dev;
-    ASD_TRY(launch_linear8(d, st, likely));
+    ASD_TRY(launch_linear8(d, st, false, likely));
   }
   return ASD_OK;
 }

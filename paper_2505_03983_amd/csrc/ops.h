@@ -56,7 +56,8 @@ __device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gr
 asd_status launch_rms_norm(const asd_norm& p, hipStream_t st);
 asd_status launch_quantize_rows(const asd_norm& p, hipStream_t st);
 // likely: rows to expect, where the device knows their number (0: all): which kernel suits, nothing else
-asd_status launch_linear8(const asd_linear8& p, hipStream_t st, int likely = 0);
+// split: the workspace has room for partial sums, where few tiles have long ones
+asd_status launch_linear8(const asd_linear8& p, hipStream_t st, bool split, int likely = 0);
 asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely = 0);
 // out[m][n] = sum over k of x[m][k] w[n][k]: bf16 rows of whole 16 bytes, side by side, fp32 results
 asd_status launch_linear_bf16(const void* x, const void* w, float* out, int rows, int cols, int channels, const int32_t* rows_used,

@@ -35,8 +35,9 @@ struct SumEpi {
   int64_t ld, ld2;
   int N, first_rows, second;   // rows 0 .. first_rows - 1 and second .. second + first_rows - 1 are stored
   bool wide;
+  __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kSplit = false;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -63,6 +64,43 @@ struct SumEpi {
   }
 };
 
+// Partial sums of a launch that splits k: part [split][rows][N] (S: float or int), added up in order by finish_kernel.
+template <class S>
+struct PartEpi {
+  S* out;
+  int64_t part_stride;
+  int N;
+  bool wide;
+  __host__ __device__ __forceinline__ int columns() const { return N; }
+  typedef S Out;
+  static constexpr bool kGated = false, kSplit = true;
+  static constexpr int kOutputs = 1;
+  struct Row {};
+  __device__ __forceinline__ Row row(int) const { return Row{}; }
+  struct Cols {};
+  __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
+  struct Extra {};
+  __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
+  __device__ __forceinline__ void values(Row, Cols, Extra, int, const S* a, const S*, S (&v)[1][4]) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[0][r] = a[r];
+  }
+  __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + (int64_t)m * N, n, N, v); }
+  __device__ __forceinline__ void store1(int m, int n, S v) const {
+    if (n < N) out[(int64_t)m * N + n] = v;
+  }
+};
+template <class S, class Epi>
+__global__ __launch_bounds__(256) void finish_kernel(const S* __restrict__ part, int64_t stride, int splits, int rows, const int32_t* rows_used, Epi epi) {
+  const int N = epi.columns(), M = rows_used ? min(max(*rows_used, 0), rows) : rows;
+  const int64_t at = workgroup() * 256 + threadIdx.x;
+  const int64_t m = at / N;
+  if (m >= M) return;
+  S s = part[at];
+  for (int z = 1; z < splits; ++z) s += part[z * stride + at];
+  epi.one((int)m, (int)(at - m * N), s, s);
+}
+
 // out = sum x_scale w_scale + bias
 template <class T>
 struct Scaled8Epi {
@@ -73,8 +111,9 @@ struct Scaled8Epi {
   const float* bias;   // or NULL
   int N;
   bool wide;
+  __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kSplit = false;
   static constexpr int kOutputs = 1;
   struct Cols {
     float s[4], b[4];
@@ -127,8 +166,9 @@ struct GatedEpi {
   int64_t ld;
   int N, act;
   bool wide;
+  __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = true;
+  static constexpr bool kGated = true, kSplit = false;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -156,8 +196,9 @@ struct Gated8Epi {
   const float* up_scale;
   int N, act;
   bool wide;
+  __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = true;
+  static constexpr bool kGated = true, kSplit = false;
   static constexpr int kOutputs = 1;
   struct Cols {
     float g[4], u[4];
@@ -198,8 +239,9 @@ struct GatedGradEpi {
   int64_t ld_dh;
   int N, act;
   bool dh_wide;   // runs of four of dh lie on 8 bytes
+  __host__ __device__ __forceinline__ int columns() const { return Np; }
   typedef T Out;
-  static constexpr bool kGated = true;
+  static constexpr bool kGated = true, kSplit = false;
   static constexpr int kOutputs = 2;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -231,6 +273,16 @@ struct GatedGradEpi {
   }
   static constexpr bool wide = true;
   __device__ __forceinline__ void store1(int, int, T) const {}
+  __device__ __forceinline__ void one(int m, int n, float g, float u) const {
+    float value = 0.f, slope = 0.f, d = 0.f;
+    if (n < N) {
+      d = (float)dh[m * ld_dh + n];
+      act_both(act, g, &value, &slope);
+    }
+    T* row = dgu + (int64_t)m * 2 * Np + n;
+    row[0] = n < N ? (T)(d * u * slope) : (T)0.f;
+    row[Np] = n < N ? (T)(d * value) : (T)0.f;
+  }
   __device__ __forceinline__ void store(int which, int m, int n, uint4 v) const {
     if (n < Np) *reinterpret_cast<uint4*>(dgu + (int64_t)m * 2 * Np + which * Np + n) = v;
   }
@@ -317,7 +369,7 @@ typedef RowsCfg<128, 128, 2, 2, 128, 4> Rows128;
 typedef RowsCfg<64, 128, 2, 2, 128, 5> Rows64;
 
 template <class E, class Cfg, class Epi>
-static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st) {
+static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st, int splits = 1) {
   void (*kern)(RowsProduct, int, int, Epi);
   if constexpr (std::is_same<Cfg, Rows256>::value) kern = gemm_rows_big_kernel<E, Epi>;
   else kern = gemm_rows_kernel<E, Cfg, Epi>;
@@ -332,18 +384,20 @@ static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st
   }
   const int tm = (int)ceil_div(p.M, Cfg::BM), tn = (int)ceil_div(p.N, Epi::kGated ? Cfg::BN / 2 : Cfg::BN);
   const int64_t grid = ceil_div((int64_t)tm * tn, 8) * 8;
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Cfg::THREADS), Cfg::PIPE_BYTES, st, p, tm, tn, e);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid, (unsigned)splits), dim3(Cfg::THREADS), Cfg::PIPE_BYTES, st, p, tm, tn, e);
   return hipGetLastError();
 }
 
 // Which kernel: the least of the estimates below, in microseconds.  A tile takes f + k per 128 bytes of k, a workgroup has its CU
-// to itself, and from the third round on the CUs no longer finish together.  Fitted to 24 .. 2000 rows by 1024 .. 11000 channels of
-// 1024 .. 11008 numbers, 8-bit products and bf16 gated units (both matrices' channels count), operands from the Infinity Cache.
-// Few rows: the weights' bytes at a rate that falls with the rows a workgroup holds, each 64 rows reading them again.
-// Measured, few / 64 x 128 / 128 x 128 / 256 x 256: 8 bits, 4096 channels of 4096: 8 rows 7.1 / 12.4 / 13.8 / -, 64 rows 13.6 / 12.6 /
-// 14.9 / -, 1000 rows - / 28 / 23 / 47, 4000 rows - / 110 / 83 / 59; gated bf16, 4096 channels of 4096: 8 rows 18 / 20 / 23 / -, 64 rows
-// 31 / 20 / 24 / -, 400 rows - / 42 / 32 / 82, 2000 rows - / 177 / 129 / 108.  Of those 80 calls the rule misses the fastest kernel
-// by more than a tenth in two.
+// to itself, and from the third round on the CUs no longer finish together.  Few rows: a workgroup of 16 channels pulls its rows of
+// both operands at 32 KB a microsecond.  Fitted to 1 .. 4000 rows by 320 .. 11000 channels of 1024 .. 14848 numbers, 8-bit products and
+// bf16 gated units (both matrices' channels count), operands from the Infinity Cache.
+// Measured, few / 64 x 128 / 128 x 128 / 256 x 256: 8 bits, 4096 channels of 4096: 1 row 6.4 / 12.6 / 14.1 / -, 64 rows 13.4 / 12.7 /
+// 14.8 / -, 1000 rows - / 29 / 24 / 48, 4000 rows - / 110 / 83 / 59; gated bf16, 4096 channels of 4096: 1 row 16 / 20 / 23 / -, 64 rows
+// 30 / 21 / 24 / -, 400 rows - / 42 / 32 / 82, 2000 rows - / 177 / 129 / 108.  Of 140 such calls the rule misses the fastest kernel by
+// more than a quarter in none, by more than a tenth in nine.
+// Split k (pick_split), where the caller has room for the parts: 768 channels of 14848 in 8 bits, 64 rows 17.5 -> 12.9, 200 rows 33 ->
+// 15.5; 4096 of 11008, 64 rows 28.6 -> 17.5.
 struct RowsCost {
   int bm, bn;
   float f, k;
@@ -351,31 +405,68 @@ struct RowsCost {
 };
 constexpr RowsCost kRowsCost[3] = {{256, 256, 8.f, 1.14f, 1.15f}, {128, 128, 4.5f, 0.34f, 1.3f}, {64, 128, 4.5f, 0.27f, 1.1f}};
 constexpr int kFewRows = 64;
-constexpr float kFewRate[3] = {4.6f, 2.9f, 1.8f};   // TB/s; up to 16, 32, 64 rows
 
-// 0 .. 2: a tile; 3 .. 5: few rows, 16 .. 64 at a time
-static float kernel_us(int kernel, int M, int64_t n, int64_t kb) {
-  if (kernel >= 3) return 3.f + 1e-6f * (float)n * (float)kb / kFewRate[kernel - 3] * (float)ceil_div(M, 16 << (kernel - 3));
+// Kernel 0 .. 2: a tile; 3 .. 5: few rows, 16, 32 or 64 a workgroup.  splits: workgroups that share a tile's k.
+static float kernel_us(int kernel, int M, int64_t n, int64_t kb, int splits = 1) {
+  if (kernel >= 3) {   // a workgroup pulls its rows of both operands at 32 KB a microsecond, the chip at 4.8 MB
+    const int rows = 16 << (kernel - 3);
+    const float wgs = (float)(ceil_div(M, rows) * ceil_div(n, 16)), bytes = (float)kb * (float)(16 + std::min(M, rows));
+    return 3.f + std::max(1.f, wgs / 256.f) * bytes / 32e3f;
+  }
   const RowsCost& c = kRowsCost[kernel];
-  const int64_t tiles = ceil_div(M, c.bm) * ceil_div(n, c.bn);
+  const int64_t tiles = ceil_div(M, c.bm) * ceil_div(n, c.bn) * splits;
   float rounds = (float)ceil_div(tiles, 256);
   if (rounds > 2.f) rounds = 0.4f * rounds + 0.6f * (float)tiles / 256.f;
-  return rounds * (tiles > 256 ? c.full : 1.f) * (c.f + c.k * (float)ceil_div(kb, 128));
+  const float t = rounds * (tiles > 256 ? c.full : 1.f) * (c.f + c.k * (float)ceil_div(kb, 128 * splits));
+  // the parts are written, read again and added by a kernel of its own
+  return splits == 1 ? t : t + 5.f + 8e-6f * (float)splits * (float)M * (float)n / 4.f;
 }
 static int pick_product(int M, int64_t n, int64_t kb) {
   int best = 0;
   for (int i = 1; i < 3; ++i)
     if (kernel_us(i, M, n, kb) < kernel_us(best, M, n, kb)) best = i;
-  const int few = M <= 16 ? 3 : M <= 32 ? 4 : 5;
-  return M <= kFewRows && kernel_us(few, M, n, kb) < kernel_us(best, M, n, kb) ? few : best;
+  for (int few = 3; M <= kFewRows && few < 6; ++few)
+    if (kernel_us(few, M, n, kb) < kernel_us(best, M, n, kb)) best = few;
+  return best;
 }
 int product_pick(int rows, int64_t channels, int64_t kb) { return pick_product(rows, channels, kb); }
 double product_us(int rows, int most, int64_t channels, int64_t kb) { return kernel_us(pick_product(most, channels, kb), rows, channels, kb); }
 
+// How a product whose caller has room for partial sums splits k: few tiles and long sums.  {1, 0}: not at all.
+struct Split {
+  int splits, tile;
+};
+constexpr int kMaxSplits = 16;
+static Split pick_split(int M, int64_t n, int64_t kb) {
+  Split best{1, 0};
+  float least = 0.9f * kernel_us(pick_product(M, n, kb), M, n, kb);   // (a second kernel for less is not worth its place)
+  for (int tile = 0; tile < 3; ++tile)
+    for (int s = 2; s <= kMaxSplits && kb >= (int64_t)s * 1024; ++s)
+      if (const float t = kernel_us(tile, M, n, kb, s); t < least) {
+        least = t;
+        best = {s, tile};
+      }
+  return best;
+}
+
 template <class E, int MT, class Epi>
 static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st) {
-  const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)ceil_div(p.M, 16 * MT));
+  const dim3 grid((unsigned)ceil_div(e.columns(), 16), (unsigned)ceil_div(p.M, 16 * MT));
   hipLaunchKernelGGL((gemm_few_rows_kernel<E, MT, Epi>), grid, dim3(512), 0, st, p, e);
+  return hipGetLastError();
+}
+
+// part: room for splits * M * N sums
+template <class E, class Epi>
+static hipError_t launch_split(const RowsProduct& p, const Epi& e, Split sp, void* part, hipStream_t st) {
+  typedef typename E::Sum S;
+  const PartEpi<S> pe{static_cast<S*>(part), (int64_t)p.M * p.N, p.N, (p.N & 3) == 0};
+  hipError_t err = sp.tile == 0   ? launch_rows<E, Rows256>(p, pe, st, sp.splits)
+                   : sp.tile == 1 ? launch_rows<E, Rows128>(p, pe, st, sp.splits)
+                                  : launch_rows<E, Rows64>(p, pe, st, sp.splits);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL((finish_kernel<S, Epi>), grid_of(ceil_div((int64_t)p.M * p.N, 256)), dim3(256), 0, st, pe.out, pe.part_stride, sp.splits,
+                     p.M, p.rows_used, e);
   return hipGetLastError();
 }
 
@@ -383,11 +474,9 @@ template <class E, class Epi>
 static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st, int likely = 0) {
   int pick = pick_product(likely > 0 ? std::min(likely, p.M) : p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
   if (pick >= 3 && ceil_div(p.M, 16 << (pick - 3)) > 65535) pick = 2;   // (few are likely of very many: a dimension of the grid)
-  if constexpr (Epi::kOutputs == 1) {
-    if (pick == 3) return launch_few<E, 1>(p, e, st);
-    if (pick == 4) return launch_few<E, 2>(p, e, st);
-    if (pick == 5) return launch_few<E, 4>(p, e, st);
-  }
+  if (pick == 3) return launch_few<E, 1>(p, e, st);
+  if (pick == 4) return launch_few<E, 2>(p, e, st);
+  if (pick == 5) return launch_few<E, 4>(p, e, st);
   if (pick == 0) return launch_rows<E, Rows256>(p, e, st);
   return pick == 1 ? launch_rows<E, Rows128>(p, e, st) : launch_rows<E, Rows64>(p, e, st);
 }
@@ -440,11 +529,15 @@ static int64_t k_bytes(int64_t row) { return ceil_div(row, 16) * 16; }
 // ---- the 8-bit linear layer ----------------------------------------------------------------------------------------------------
 struct Linear8Plan {
   Operand x, w;
+  Split split;
+  uint8_t* part;
   size_t bytes;
 };
-static Linear8Plan plan_linear8(const asd_linear8& p, void* ws) {
+static Linear8Plan plan_linear8(const asd_linear8& p, void* ws, bool split) {
   Carve c{static_cast<uint8_t*>(ws)};
   Linear8Plan r;
+  r.split = split ? pick_split(p.rows, p.channels, k_bytes(p.cols)) : Split{1, 0};
+  r.part = r.split.splits > 1 ? c.take(sizeof(int) * (size_t)r.split.splits * p.rows * p.channels) : nullptr;
   r.x = operand(p.x, p.rows, p.cols, p.ld_x, 1, &c);
   r.w = operand(p.w, p.channels, p.cols, p.ld_w, 1, &c);
   r.bytes = c.used;
@@ -455,12 +548,13 @@ template <class T>
 static asd_status run_linear8(const asd_linear8& p, const Linear8Plan& o, hipStream_t st, int likely) {
   const RowsProduct g{o.x.p, o.w.p, nullptr, o.x.pitch, o.w.pitch, 0, p.rows, p.channels, k_bytes(p.cols), p.rows_used};
   const Scaled8Epi<T> e{static_cast<T*>(p.out), p.ld_out, p.x_scale, p.w_scale, p.bias, p.channels, on16(p.out, p.ld_out, sizeof(T))};
-  ASD_HIP(launch_product<ElemI8>(g, e, st, likely));
+  if (o.split.splits > 1) ASD_HIP(launch_split<ElemI8>(g, e, o.split, o.part, st));
+  else ASD_HIP(launch_product<ElemI8>(g, e, st, likely));
   return ASD_OK;
 }
 
-asd_status launch_linear8(const asd_linear8& p, hipStream_t st, int likely) {
-  const Linear8Plan o = plan_linear8(p, p.workspace);
+asd_status launch_linear8(const asd_linear8& p, hipStream_t st, bool split, int likely) {
+  const Linear8Plan o = plan_linear8(p, p.workspace, split);
   ASD_HIP(bring({&o.x, &o.w}, st));
   return p.out_type == ASD_F32    ? run_linear8<float>(p, o, st, likely)
          : p.out_type == ASD_BF16 ? run_linear8<__bf16>(p, o, st, likely)
@@ -523,6 +617,8 @@ struct GatedGradPlan {
   int Np;        // channels, padded to whole stages of k
   int64_t Mp;    // rows, likewise
   uint8_t *dgu, *dgu_t, *w_t, *x_t;
+  Split dx, dw;
+  uint8_t* part;   // partial sums of the one product, then of the other
   size_t bytes;
 };
 static GatedGradPlan plan_gated_grad(const asd_gated& p) {
@@ -535,6 +631,10 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   r.w_t = p.dx ? c.take((size_t)2 * p.cols * 2 * r.Np) : nullptr;
   r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * r.Mp) : nullptr;
   r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * r.Mp) : nullptr;
+  r.dx = p.dx ? pick_split(p.rows, p.cols, 4 * (int64_t)r.Np) : Split{1, 0};
+  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, 2 * r.Mp) : Split{1, 0};
+  const size_t dx_sums = r.dx.splits > 1 ? (size_t)r.dx.splits * p.rows * p.cols : 0, dw_sums = r.dw.splits > 1 ? (size_t)r.dw.splits * 2 * r.Np * p.cols : 0;
+  r.part = c.take(sizeof(float) * std::max(dx_sums, dw_sums));
   r.bytes = c.used;
   return r;
 }
@@ -564,7 +664,7 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
     ASD_HIP(transpose16(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, 2 * o.Np, st));
     const RowsProduct g{o.dgu, o.w_t, nullptr, 4 * (int64_t)o.Np, 4 * (int64_t)o.Np, 0, p.rows, p.cols, 4 * (int64_t)o.Np, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
-    ASD_HIP(launch_product<E>(g, s, st));
+    ASD_HIP(o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st) : launch_product<E>(g, s, st));
   }
   if (p.dw_gate) {
     ASD_HIP(transpose16(o.dgu, 2 * o.Np, p.rows, 2 * o.Np, o.dgu_t, o.Mp, st));
@@ -572,7 +672,7 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
     const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * o.Mp, 2 * o.Mp, 0, 2 * o.Np, p.cols, 2 * o.Mp, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
                       on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
-    ASD_HIP(launch_product<E>(g, s, st));
+    ASD_HIP(o.dw.splits > 1 ? launch_split<E>(g, s, o.dw, o.part, st) : launch_product<E>(g, s, st));
   }
   return ASD_OK;
 }
@@ -609,7 +709,7 @@ static asd_status check_linear8(const asd_linear8* p) {
                       {"bias", p->bias, 1, p->channels, p->channels, 4, false},
                       {"rows_used", p->rows_used, 1, 1, 1, 4, false}};
   ASD_TRY(check_mats(m, 8));
-  return check_workspace(p->workspace, p->workspace_bytes, plan_linear8(*p, nullptr).bytes);
+  return check_workspace(p->workspace, p->workspace_bytes, plan_linear8(*p, nullptr, true).bytes);
 }
 
 static asd_status check_gated(const asd_gated* p, bool backward) {
@@ -661,12 +761,12 @@ using namespace asd;
 extern "C" {
 
 size_t asd_linear_i8_workspace(const asd_linear8* p) {
-  return !p || p->rows < 1 || p->cols < 1 || p->channels < 1 ? 0 : plan_linear8(*p, nullptr).bytes;
+  return !p || p->rows < 1 || p->cols < 1 || p->channels < 1 ? 0 : plan_linear8(*p, nullptr, true).bytes;
 }
 
 asd_status asd_linear_i8(const asd_linear8* p, void* stream) {
   ASD_TRY(check_linear8(p));
-  return p->rows ? launch_linear8(*p, (hipStream_t)stream) : ASD_OK;
+  return p->rows ? launch_linear8(*p, (hipStream_t)stream, true) : ASD_OK;
 }
 
 size_t asd_gated_ff_workspace(const asd_gated* p) {

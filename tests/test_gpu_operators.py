@@ -198,7 +198,7 @@ SIZES = [(1, 1, 1), (1, 16, 3), (2, 4096, 48), (1, 1000, 777), (16, 272, 16), (1
          (1025, 333, 2051), (2048, 512, 4096)]
 
 
-@pytest.mark.parametrize("rows, cols, channels", SIZES + [(3, 131071, 20), (70, 131071, 70)])
+@pytest.mark.parametrize("rows, cols, channels", SIZES + [(3, 131071, 20), (70, 131071, 70), (300, 16400, 200), (64, 14848, 768)])
 def test_linear_i8(rows, cols, channels):
     g = gen(rows + channels)
     x, w = rand_i8(g, rows, cols), rand_i8(g, channels, cols)
@@ -283,7 +283,8 @@ def test_gated_of_integers(rows, cols, channels, t, act):
 
 
 @pytest.mark.parametrize("rows, cols, channels", [(1, 1, 1), (2, 16, 64), (5, 7, 9), (64, 64, 64), (65, 130, 67), (100, 1000, 300),
-                                                  (200, 72, 129), (130, 520, 1030), (1000, 256, 512), (700, 1100, 1500)])
+                                                  (200, 72, 129), (130, 520, 1030), (1000, 256, 512), (700, 1100, 1500),
+                                                  (5000, 100, 140), (20, 72, 6000), (9001, 640, 72), (16, 33, 47)])
 @pytest.mark.parametrize("t, act", [(BF16, "silu"), (F16, "gelu")])
 def test_gated_gradient(rows, cols, channels, t, act):
     g = gen(rows + cols)
