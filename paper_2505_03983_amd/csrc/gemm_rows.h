@@ -120,6 +120,17 @@ __device__ __forceinline__ bool rows_tile(int tiles_m, int tiles_n, int* tm, int
   return true;
 }
 
+// LDS of a wavefront's transposed results, and of a kernel.
+template <class Cfg, class Epi>
+constexpr int rows_turned_bytes() {
+  return Epi::kTurned ? Epi::kOutputs * (Cfg::WN / 2) * Cfg::WM * 2 : 0;
+}
+template <class Cfg, class Epi, int B>
+constexpr int rows_lds_bytes() {
+  const int parked = Cfg::NW * (B * Epi::kOutputs * (Cfg::WN / (Epi::kGated ? 2 : 1)) * (int)sizeof(typename Epi::Out) + rows_turned_bytes<Cfg, Epi>());
+  return parked > Cfg::PIPE_BYTES ? parked : Cfg::PIPE_BYTES;
+}
+
 // Epilogue.  acc[j][i]: blocks of B x B results (B = 32 or 16 by the matrix instruction), channels by rows; a lane holds, of its
 // row of a block, four channels at 4 (lane / B), and with B = 32 those 8, 16 and 24 further on.  The results go through LDS, in
 // the output's type, 64 columns a wavefront or 32 where two factors become one, so that rows leave in whole runs; LDS slots of 16
@@ -135,10 +146,15 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
   typedef typename Epi::Out Out;
   constexpr int COLS = Cfg::WN / (GATED ? 2 : 1), OB = (int)sizeof(Out), OUTS = Epi::kOutputs;
   constexpr int ROWB = OUTS * COLS * OB, SL = ROWB / 16;    // bytes and slots of a parked row: one output after the other
-  static_assert(NW * B * ROWB <= Cfg::PIPE_BYTES, "parked results");
+  static_assert(rows_lds_bytes<Cfg, Epi, B>() <= 160 * 1024, "LDS of a CU");
   static_assert(SL >= 2 && SL <= 64 && (SL & (SL - 1)) == 0, "slots of a parked row");
   constexpr int FACTOR = GATED ? 32 / B : 0;                // blocks from a gate's to the matching up's
   uint8_t* park = lds + wave * (B * ROWB);
+  // the transposed copy, in 16-bit numbers: the wavefront's columns, WM rows each, behind the parked rows of all wavefronts; chunks of
+  // eight rows are permuted by the column for the banks
+  constexpr int CH = Cfg::WM / 8;
+  uint8_t* turned = lds + NW * (B * ROWB) + wave * rows_turned_bytes<Cfg, Epi>();
+  auto turned_key = [](int col) { return (col >> 2) * 2 & (CH - 1); };
   const int col0 = n0 + wn * COLS;                          // channel of the wavefront's first column
   auto column = [&](int j, int q) { return (GATED ? j * B / 64 * 32 + j * B % 32 : j * B) + (B == 32 ? 8 * q : 0) + 4 * part; };
   // what belongs to columns is the same for all rows: loaded once
@@ -162,7 +178,9 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
 #pragma unroll
   for (int i = 0; i < MB; ++i) {
     const int mrow = m0 + wm * Cfg::WM + i * B;
-    if (mrow >= M) break;
+    bool over = mrow >= M;
+    if constexpr (Epi::kTurned) over = mrow >= epi.turned_rows(M);
+    if (over) break;
     if (i + 1 < MB) fetch(i + 1);
     const int m = min(mrow + lrow, M - 1);
     const auto rc = epi.row(m);
@@ -183,6 +201,16 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
 #pragma unroll
         for (int o = 0; o < OUTS; ++o) {
           const int byte = (o * COLS + c) * OB, sl = (byte >> 4) ^ (lrow & (SL - 1));
+          if constexpr (Epi::kTurned) {
+            if (epi.turned) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int col = o * COLS + c + r, at = i * B + lrow;
+                *reinterpret_cast<Out*>(turned + col * (Cfg::WM * 2) + (((at >> 3) ^ turned_key(col)) * 16) + (at & 7) * 2) =
+                    mrow + lrow < M ? v[o][r] : (Out)0.f;
+              }
+            }
+          }
           if constexpr (OB == 2) *reinterpret_cast<uint2*>(park + lrow * ROWB + sl * 16 + (byte & 15)) = *reinterpret_cast<const uint2*>(v[o]);
           else *reinterpret_cast<uint4*>(park + lrow * ROWB + sl * 16) = *reinterpret_cast<const uint4*>(v[o]);
         }
@@ -205,6 +233,16 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
       const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
       if (lane < RPI * SL && mrow + r < M) epi.store(sl / (SL / OUTS), mrow + r, col0 + sl % (SL / OUTS) * (16 / OB), v);
     }
+  }
+  if constexpr (Epi::kTurned) {
+    static_assert(OB == 2, "16-bit numbers");
+    if (epi.turned)
+#pragma unroll 4
+      for (int e = lane; e < OUTS * COLS * CH; e += 64) {
+        const int col = e / CH, ch = e % CH;
+        const uint4 v = *reinterpret_cast<const uint4*>(turned + col * (Cfg::WM * 2) + ((ch ^ turned_key(col)) * 16));
+        epi.store_turned(col / COLS, m0 + wm * Cfg::WM + ch * 8, col0 + col % COLS, M, v);
+      }
   }
 }
 

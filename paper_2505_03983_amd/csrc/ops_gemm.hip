@@ -37,7 +37,7 @@ struct SumEpi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = false, kSplit = false;
+  static constexpr bool kGated = false, kSplit = false, kTurned = false;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -73,7 +73,7 @@ struct PartEpi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef S Out;
-  static constexpr bool kGated = false, kSplit = true;
+  static constexpr bool kGated = false, kSplit = true, kTurned = false;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -113,7 +113,7 @@ struct Scaled8Epi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = false, kSplit = false;
+  static constexpr bool kGated = false, kSplit = false, kTurned = false;
   static constexpr int kOutputs = 1;
   struct Cols {
     float s[4], b[4];
@@ -168,7 +168,7 @@ struct GatedEpi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = true, kSplit = false;
+  static constexpr bool kGated = true, kSplit = false, kTurned = false;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -198,7 +198,7 @@ struct Gated8Epi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = true, kSplit = false;
+  static constexpr bool kGated = true, kSplit = false, kTurned = false;
   static constexpr int kOutputs = 1;
   struct Cols {
     float g[4], u[4];
@@ -230,7 +230,8 @@ struct Gated8Epi {
 };
 
 // dg = dh u act'(g) and du = dh act(g), side by side: dgu [rows][2 Np], zeros in the columns N .. Np - 1 of either half.  Rounded
-// to the operands' type, as the products that follow take them.
+// to the operands' type, as the products that follow take them; the tiles store them transposed, too, for the one that contracts over
+// rows (as a pass of its own 230 us of 8192 x 2 * 16384, and a launch).
 template <class T>
 struct GatedGradEpi {
   T* dgu;
@@ -239,9 +240,15 @@ struct GatedGradEpi {
   int64_t ld_dh;
   int N, act;
   bool dh_wide;   // runs of four of dh lie on 8 bytes
+  T* turned;      // NULL, or the same transposed: [2 Np][Mp], zeros in the columns M .. Mp - 1
+  int64_t Mp;
+  __device__ __forceinline__ int turned_rows(int M) const { return turned ? (int)Mp : M; }
+  __device__ __forceinline__ void store_turned(int which, int m, int n, int, uint4 v) const {
+    if (n < Np && m < Mp) *reinterpret_cast<uint4*>(turned + ((int64_t)which * Np + n) * Mp + m) = v;
+  }
   __host__ __device__ __forceinline__ int columns() const { return Np; }
   typedef T Out;
-  static constexpr bool kGated = true, kSplit = false;
+  static constexpr bool kGated = true, kSplit = false, kTurned = true;
   static constexpr int kOutputs = 2;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -329,11 +336,31 @@ __global__ __launch_bounds__(64 * kCopyRows) void pack_rows_kernel(RowsCopies al
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
-// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).
-__global__ __launch_bounds__(256) void transpose16_kernel(const uint16_t* __restrict__ src, int64_t ld, int rows, int cols, int wide,
-                                                          uint16_t* __restrict__ dst, int64_t dst_ld) {
+// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to three matrices a launch.
+struct Transpose16 {
+  const uint16_t* src;
+  uint16_t* dst;
+  int64_t ld, dst_ld;
+  int rows, cols;
+  bool wide;   // rows on 16 bytes
+};
+struct Transposes16 {
+  Transpose16 t[3];
+  int64_t first[3];   // its first workgroup
+  int n;
+};
+__global__ __launch_bounds__(256) void transpose16_kernel(Transposes16 all) {
+  int i = 0;
+  while (i + 1 < all.n && workgroup() >= all.first[i + 1]) ++i;
+  const uint16_t* src = all.t[i].src;
+  uint16_t* dst = all.t[i].dst;
+  const int64_t ld = all.t[i].ld, dst_ld = all.t[i].dst_ld;
+  const int rows = all.t[i].rows, cols = all.t[i].cols;
+  const bool wide = all.t[i].wide;
+  const unsigned at = (unsigned)(workgroup() - all.first[i]), across = (unsigned)(cols + 63) / 64;
+  if (at / across * 64 >= (unsigned)rows) return;   // (the grid's last row of workgroups)
   __shared__ uint16_t tile[64][72];   // (rows 144 bytes apart: columns of eight rows fall on different banks)
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, t = threadIdx.x;
+  const int r0 = (int)(at / across) * 64, c0 = (int)(at % across) * 64, t = threadIdx.x;
 #pragma unroll
   for (int pass = 0; pass < 2; ++pass) {
     const int r = pass * 32 + (t >> 3), c = (t & 7) * 8;
@@ -370,21 +397,23 @@ typedef RowsCfg<64, 128, 2, 2, 128, 5> Rows64;
 
 template <class E, class Cfg, class Epi>
 static hipError_t launch_rows(const RowsProduct& p, const Epi& e, hipStream_t st, int splits = 1) {
+  constexpr bool BIG = std::is_same<Cfg, Rows256>::value;
+  constexpr int LDS = rows_lds_bytes<Cfg, Epi, BIG ? 16 : 32>();
   void (*kern)(RowsProduct, int, int, Epi);
-  if constexpr (std::is_same<Cfg, Rows256>::value) kern = gemm_rows_big_kernel<E, Epi>;
+  if constexpr (BIG) kern = gemm_rows_big_kernel<E, Epi>;
   else kern = gemm_rows_kernel<E, Cfg, Epi>;
   static std::atomic<uint64_t> ready{0};   // devices whose limit of dynamic LDS has been raised for this kernel
   int dev = 0;
   hipError_t err = hipGetDevice(&dev);
   if (err != hipSuccess) return err;
   if (!(ready.load() >> (dev & 63) & 1)) {
-    err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::PIPE_BYTES);
+    err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (err != hipSuccess) return err;
     ready.fetch_or(1ull << (dev & 63));
   }
   const int tm = (int)ceil_div(p.M, Cfg::BM), tn = (int)ceil_div(p.N, Epi::kGated ? Cfg::BN / 2 : Cfg::BN);
   const int64_t grid = ceil_div((int64_t)tm * tn, 8) * 8;
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid, (unsigned)splits), dim3(Cfg::THREADS), Cfg::PIPE_BYTES, st, p, tm, tn, e);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid, (unsigned)splits), dim3(Cfg::THREADS), LDS, st, p, tm, tn, e);
   return hipGetLastError();
 }
 
@@ -639,10 +668,18 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   return r;
 }
 
-static hipError_t transpose16(const void* src, int64_t ld, int rows, int cols, uint8_t* dst, int64_t dst_ld, hipStream_t st) {
-  const dim3 grid((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 64));
-  hipLaunchKernelGGL(transpose16_kernel, grid, dim3(256), 0, st, static_cast<const uint16_t*>(src), ld, rows, cols, on16(src, ld, 2) ? 1 : 0,
-                     reinterpret_cast<uint16_t*>(dst), dst_ld);
+static Transpose16 transposed(const void* src, int64_t ld, int rows, int cols, uint8_t* dst, int64_t dst_ld) {
+  return Transpose16{static_cast<const uint16_t*>(src), reinterpret_cast<uint16_t*>(dst), ld, dst_ld, rows, cols, on16(src, ld, 2)};
+}
+static hipError_t transpose16(std::initializer_list<Transpose16> list, hipStream_t st) {
+  Transposes16 all{};
+  int64_t grid = 0;
+  for (const Transpose16& t : list) {
+    all.first[all.n] = grid;
+    all.t[all.n++] = t;
+    grid += ceil_div(t.cols, 64) * ceil_div(t.rows, 64);
+  }
+  hipLaunchKernelGGL(transpose16_kernel, grid_of(grid), dim3(256), 0, st, all);
   return hipGetLastError();
 }
 
@@ -656,19 +693,21 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   const GatedGradPlan o = plan_gated_grad(p);
   ASD_HIP(bring({&o.in.x, &o.in.g, &o.in.u}, st));
   T* dgu = reinterpret_cast<T*>(o.dgu);
+  const bool few = pick_product(p.rows, 2 * (int64_t)p.channels, k_bytes(2 * (int64_t)p.cols)) >= 3;   // (that kernel transposes nothing)
   const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act,
-                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0};
+                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
   ASD_HIP(launch_product<E>(gated_product(p, o.in), e, st));
+  const Transpose16 gate = transposed(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, 2 * o.Np),
+                    up = transposed(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t ? o.w_t + 2 * (size_t)o.Np : nullptr, 2 * o.Np),
+                    x = transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t, o.Mp);
+  ASD_HIP(!p.dw_gate ? transpose16({gate, up}, st) : !p.dx ? transpose16({x}, st) : transpose16({gate, up, x}, st));
   if (p.dx) {
-    ASD_HIP(transpose16(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, 2 * o.Np, st));
-    ASD_HIP(transpose16(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, 2 * o.Np, st));
     const RowsProduct g{o.dgu, o.w_t, nullptr, 4 * (int64_t)o.Np, 4 * (int64_t)o.Np, 0, p.rows, p.cols, 4 * (int64_t)o.Np, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
     ASD_HIP(o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st) : launch_product<E>(g, s, st));
   }
   if (p.dw_gate) {
-    ASD_HIP(transpose16(o.dgu, 2 * o.Np, p.rows, 2 * o.Np, o.dgu_t, o.Mp, st));
-    ASD_HIP(transpose16(p.x, p.ld_x, p.rows, p.cols, o.x_t, o.Mp, st));
+    if (few) ASD_HIP(transpose16({transposed(o.dgu, 2 * o.Np, p.rows, 2 * o.Np, o.dgu_t, o.Mp)}, st));
     const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * o.Mp, 2 * o.Mp, 0, 2 * o.Np, p.cols, 2 * o.Mp, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
                       on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
