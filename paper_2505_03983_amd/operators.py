@@ -1,6 +1,8 @@
 """The operators of a gated residual network (include/asd.h) on torch tensors: shapes, types and devices are checked here,
-outputs and workspaces are allocated by torch, the kernels run on the tensors' device and its current stream (or `stream`).
-Matrices may have any row pitch; their columns lie next to each other.  There is no fallback: without a GPU a call raises."""
+outputs and workspaces are allocated by torch, the kernels run on the tensors' device and its current stream.  With `stream` (a
+torch stream of that device) a call is made as under `torch.cuda.stream(stream)`: new outputs are that stream's, and the inputs have
+to be ready for it.  Matrices may have any row pitch; their columns lie next to each other.  Results carry no autograd history: the
+gradients are the *_backward calls.  There is no fallback: without a GPU a call raises."""
 import torch
 
 from . import binding
@@ -83,26 +85,26 @@ def _rows_of(x, name="x"):
     return x.shape[0], x.shape[1]
 
 
-def _launch(name, args, device, stream, workspace=True):
+def _on(stream, device):
+    """The context of a call with a stream of its own."""
+    if not isinstance(stream, torch.cuda.Stream) or stream.device != device:
+        _refuse("the stream is no torch stream of %s" % device)
+    return torch.cuda.stream(stream)
+
+
+def _launch(name, args, device, workspace=True):
     """Runs an entry on the tensors' device; its workspace is torch's, which hands memory on in the order of the stream."""
     if torch.cuda.current_device() != device.index:
         with torch.cuda.device(device):
-            return _launch(name, args, device, stream, workspace)
-    if stream is not None and getattr(stream, "device", device) != device:
-        _refuse("the stream is on %s, the tensors on %s" % (stream.device, device))
+            return _launch(name, args, device, workspace)
     ws = None
     if workspace:
         need = _entry(name + "_workspace")(args)
         if need:
-            if stream is None:
-                ws = torch.empty(need, dtype=torch.uint8, device=device)
-            else:
-                with torch.cuda.stream(stream):
-                    ws = torch.empty(need, dtype=torch.uint8, device=device)
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
             args.workspace, args.workspace_bytes = ws.data_ptr(), need
     # (the raw handle: the stream object that torch.cuda.current_stream makes takes longer than a launch)
-    raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
-    s = _entry(name)(args, raw)
+    s = _entry(name)(args, torch._C._cuda_getCurrentRawStream(device.index))
     if s != binding.ASD_OK:
         raise binding.AsdError(s, binding.last_error())
 
@@ -112,6 +114,9 @@ def rms_norm(x, gain=None, eps=1e-6, residual=None, out_type=None, out=None, sca
     """(out, scale, sum): the rows of x (+ residual) over their root mean square, times gain.  out_type torch.int8: 8-bit
     integers, and their scales; a number type (default x's): scale is None.  sum is x + residual as the next layer's residual
     stream (None without a residual, unless sum_out is given; sum_out may be x or residual)."""
+    if stream is not None:
+        with _on(stream, x.device):
+            return rms_norm(x, gain, eps, residual, out_type, out, scale, sum_out, rows_used)
     rows, cols = _rows_of(x)
     dev, t = x.device, x.dtype
     out_type = out_type or t
@@ -132,12 +137,15 @@ def rms_norm(x, gain=None, eps=1e-6, residual=None, out_type=None, out=None, sca
     else:
         scale = None
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
-    _launch("asd_rms_norm", a, dev, stream, workspace=False)
+    _launch("asd_rms_norm", a, dev, workspace=False)
     return out, scale, sum_out
 
 
 def quantize_rows(x, out=None, scale=None, rows_used=None, stream=None):
     """(out, scale): the rows of x as 8-bit integers, out * scale[:, None] being x to half a step."""
+    if stream is not None:
+        with _on(stream, x.device):
+            return quantize_rows(x, out, scale, rows_used)
     rows, cols = _rows_of(x)
     dev, t = x.device, x.dtype
     if t not in _TYPE:
@@ -147,13 +155,16 @@ def quantize_rows(x, out=None, scale=None, rows_used=None, stream=None):
     out, a.out, a.ld_out = _out(out, "out", torch.int8, dev, rows, cols, x)
     scale, a.scale = _out_vector(scale, "scale", torch.float32, dev, rows)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
-    _launch("asd_quantize_rows", a, dev, stream, workspace=False)
+    _launch("asd_quantize_rows", a, dev, workspace=False)
     return out, scale
 
 
 def rms_norm_backward(dy, total, gain=None, eps=1e-6, dsum=None, dx=None, dgain=None, stream=None):
     """(dx, dgain) from the gradient dy of the norm's output and total, the sum the norm was taken of (x itself without a
     residual).  dsum: the gradient that reaches the sum from elsewhere.  dx is the gradient of x and of residual."""
+    if stream is not None:
+        with _on(stream, total.device):
+            return rms_norm_backward(dy, total, gain, eps, dsum, dx, dgain)
     rows, cols = _rows_of(total, "total")
     dev, t = total.device, total.dtype
     if t not in _TYPE:
@@ -166,12 +177,15 @@ def rms_norm_backward(dy, total, gain=None, eps=1e-6, dsum=None, dx=None, dgain=
     a.gain = _vector(gain, "gain", t, dev, cols)
     dx, a.dx, a.ld_dx = _out(dx, "dx", t, dev, rows, cols, total)
     dgain, a.dgain = _out_vector(dgain, "dgain", t, dev, cols)
-    _launch("asd_rms_norm_backward", a, dev, stream)
+    _launch("asd_rms_norm_backward", a, dev)
     return dx, dgain
 
 
 def linear_i8(x, x_scale, w, w_scale, bias=None, out_type=torch.bfloat16, out=None, rows_used=None, stream=None):
     """x_scale[:, None] * (x @ w.T) * w_scale + bias for int8 x [rows, cols] and w [channels, cols]."""
+    if stream is not None:
+        with _on(stream, x.device):
+            return linear_i8(x, x_scale, w, w_scale, bias, out_type, out, rows_used)
     rows, cols = _rows_of(x)
     dev = x.device
     channels = w.shape[0] if w.dim() == 2 else 0
@@ -185,7 +199,7 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, out_type=torch.bfloat16, out=No
     a.bias = _vector(bias, "bias", torch.float32, dev, channels)
     out, a.out, a.ld_out = _out(out, "out", out_type, dev, rows, channels)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
-    _launch("asd_linear_i8", a, dev, stream)
+    _launch("asd_linear_i8", a, dev)
     return out
 
 
@@ -208,6 +222,9 @@ def gated_ff(x, w_gate, w_up, act="silu", x_scale=None, gate_scale=None, up_scal
              rows_used=None, stream=None):
     """act(x @ w_gate.T) * (x @ w_up.T) for bfloat16 or float16 x [rows, cols] and weights [channels, cols], or for int8 ones
     with their scales (out_type then bfloat16, the default, or float16).  act: "silu" or "gelu" (its tanh form)."""
+    if stream is not None:
+        with _on(stream, x.device):
+            return gated_ff(x, w_gate, w_up, act, x_scale, gate_scale, up_scale, out_type, out, rows_used)
     out_type = out_type or (torch.bfloat16 if x.dtype == torch.int8 else x.dtype)
     a = _gated_args(x, w_gate, w_up, act, out_type)
     dev = x.device
@@ -217,13 +234,16 @@ def gated_ff(x, w_gate, w_up, act="silu", x_scale=None, gate_scale=None, up_scal
         a.up_scale = _vector(up_scale, "up_scale", torch.float32, dev, a.channels)
     out, a.out, a.ld_out = _out(out, "out", out_type, dev, a.rows, a.channels)
     a.rows_used = _vector(rows_used, "rows_used", torch.int32, dev, 1)
-    _launch("asd_gated_ff", a, dev, stream)
+    _launch("asd_gated_ff", a, dev)
     return out
 
 
 def gated_ff_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=True, dx=None, dw_gate=None, dw_up=None,
                       stream=None):
     """(dx, dw_gate, dw_up) from dh, the gradient of gated_ff's result; None for what is not needed."""
+    if stream is not None:
+        with _on(stream, x.device):
+            return gated_ff_backward(dh, x, w_gate, w_up, act, need_dx, need_dw, dx, dw_gate, dw_up)
     a = _gated_args(x, w_gate, w_up, act, x.dtype)
     dev, t = x.device, x.dtype
     a.dh, a.ld_dh = _matrix(dh, "dh", t, dev, a.rows, a.channels)
@@ -236,5 +256,5 @@ def gated_ff_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=Tru
         dw_up, a.dw_up, a.ld_dw_up = _out(dw_up, "dw_up", t, dev, a.channels, a.cols)
     else:
         dw_gate = dw_up = None
-    _launch("asd_gated_ff_backward", a, dev, stream)
+    _launch("asd_gated_ff_backward", a, dev)
     return dx, dw_gate, dw_up

@@ -468,6 +468,28 @@ def test_graphs_and_streams():
             assert torch.equal(a, b)
 
 
+def test_calls_on_a_stream_of_their_own():
+    g = gen(6)
+    o = O()
+    x, w, dy = randn(g, 77, 333, t=BF16), randn(g, 130, 333, t=BF16, scale=0.1), randn(g, 77, 130, t=BF16)
+    q, qs = o.quantize_rows(x)
+    wq, ws = o.quantize_rows(w)
+    gain = randn(g, 333, t=BF16)
+    calls = [lambda s: o.rms_norm(x, gain, EPS, residual=x, stream=s), lambda s: o.quantize_rows(x, stream=s),
+             lambda s: o.rms_norm_backward(x, x, gain, EPS, stream=s), lambda s: o.linear_i8(q, qs, wq, ws, stream=s),
+             lambda s: o.gated_ff(x, w, w, stream=s), lambda s: o.gated_ff_backward(dy, x, w, w, stream=s)]
+    want = [c(None) for c in calls]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [c(side) for c in calls]
+    side.synchronize()
+    for a, b in zip(got, want):
+        for u, v in zip(a if isinstance(a, tuple) else (a,), b if isinstance(b, tuple) else (b,)):
+            assert (u is None and v is None) or torch.equal(u, v)
+    with pytest.raises(binding.AsdError):
+        o.quantize_rows(x, stream=side.cuda_stream)
+
+
 def test_results_do_not_depend_on_the_other_rows():
     """In a call of the same size, a row's bits are its own."""
     g = gen(4)
