@@ -4,14 +4,14 @@
 //   r = x + residual,  rstd = (mean r^2 + eps)^(-1/2),  y = r rstd gain
 //   8 bits: v = r gain, q = nearest integer to 127 v / max |v|, scale = max |v| rstd / 127
 // rstd cancels from q: the integers depend on v alone, and a tie is a tie in exact arithmetic (v = max |v| / 2 is 63.5 steps, a
-// common case with 16-bit inputs).  So the squares' sum, v and the quotient are kept in 64 bits; the quotient, a multiplication
-// by the reciprocal with one step of correction (the remainder, exact in a fused multiply-add, times the reciprocal), is the
-// correctly rounded one, exact where it has to be.  The kernels are bound by memory; the 64-bit arithmetic, some ten
-// instructions a number at half the fp32 rate, runs under the loads.
+// common case with 16-bit inputs).  So the squares' sum, v and its largest are kept in 64 bits; a quotient is formed in 32 and, next
+// to a border, again in 64: a multiplication by the reciprocal with one step of correction (the remainder, exact in a fused
+// multiply-add, times the reciprocal) is the correctly rounded one, exact where it has to be.  The kernels are bound by memory; the
+// 64-bit arithmetic of the norm, some six instructions a number at half the fp32 rate, runs under the loads of other rows, nearly
+// all of it.
 //
-// One pass: a row lies in the registers of a wavefront (up to 2048 numbers), a workgroup of four, or of sixteen; each
-// thread holds runs of eight, loaded 16 bytes at a time, or single numbers a stride apart where rows start at no multiple of
-// 16 bytes.
+// One pass: a row lies in the registers of a wavefront (up to 1024 numbers), a workgroup of four, or of sixteen; each thread holds
+// runs of eight, loaded 16 bytes at a time, or single numbers a stride apart where rows are not whole runs on 16 bytes.
 #include <math.h>
 
 #include <type_traits>
@@ -106,7 +106,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void rms_norm_kernel
   const T* x = static_cast<const T*>(p.x) + row * p.ld_x;
   const T* res = NORM && p.residual ? static_cast<const T*>(p.residual) + row * p.ld_residual : nullptr;
   const T* gain = NORM ? static_cast<const T*>(p.gain) : nullptr;
-  // (the quantiser's rows stay in their own type: half the registers, twice the rows in flight)
+  // (the quantiser's rows stay in their own type: half the registers, twice the rows in flight; 8192 x 16384 bf16 110 -> 88 us with the
+  // quotients in fp32)
   Run<typename std::conditional<NORM, float, T>::type> r[RUNS];
   Run<T> g[RUNS];
   if constexpr (!NORM) {
