@@ -240,6 +240,7 @@ struct GatedGradEpi {
   int64_t ld_dh;
   int N, act;
   bool dh_wide;   // runs of four of dh lie on 8 bytes
+  T* lo;          // (few rows) what the rounding of dgu leaves, rounded
   T* turned;      // NULL, or the same transposed: [2 Np][Mp], zeros in the columns M .. Mp - 1
   int64_t Mp;
   __device__ __forceinline__ int turned_rows(int M) const { return turned ? (int)Mp : M; }
@@ -286,9 +287,15 @@ struct GatedGradEpi {
       d = (float)dh[m * ld_dh + n];
       act_both(act, g, &value, &slope);
     }
-    T* row = dgu + (int64_t)m * 2 * Np + n;
-    row[0] = n < N ? (T)(d * u * slope) : (T)0.f;
-    row[Np] = n < N ? (T)(d * value) : (T)0.f;
+    const int64_t at = (int64_t)m * 2 * Np + n;
+    const float v[2] = {d * u * slope, d * value};
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+      const T hi = n < N ? (T)v[o] : (T)0.f;
+      dgu[at + o * Np] = hi;
+      const float left = v[o] - (float)hi;
+      lo[at + o * Np] = n < N && fabsf(left) < INFINITY ? (T)left : (T)0.f;   // (nothing is left of an infinity)
+    }
   }
   __device__ __forceinline__ void store(int which, int m, int n, uint4 v) const {
     if (n < Np) *reinterpret_cast<uint4*>(dgu + (int64_t)m * 2 * Np + which * Np + n) = v;
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(64 * kCopyRows) void pack_rows_kernel(RowsCopies al
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
-// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to three matrices a launch.
+// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to four matrices a launch.
 struct Transpose16 {
   const uint16_t* src;
   uint16_t* dst;
@@ -345,8 +352,8 @@ struct Transpose16 {
   bool wide;   // rows on 16 bytes
 };
 struct Transposes16 {
-  Transpose16 t[3];
-  int64_t first[3];   // its first workgroup
+  Transpose16 t[4];
+  int64_t first[4];   // its first workgroup
   int n;
 };
 __global__ __launch_bounds__(256) void transpose16_kernel(Transposes16 all) {
@@ -450,10 +457,14 @@ static float kernel_us(int kernel, int M, int64_t n, int64_t kb, int splits = 1)
   // the parts are written, read again and added by a kernel of its own
   return splits == 1 ? t : t + 5.f + 8e-6f * (float)splits * (float)M * (float)n / 4.f;
 }
-static int pick_product(int M, int64_t n, int64_t kb) {
+static int best_tile(int M, int64_t n, int64_t kb) {
   int best = 0;
   for (int i = 1; i < 3; ++i)
     if (kernel_us(i, M, n, kb) < kernel_us(best, M, n, kb)) best = i;
+  return best;
+}
+static int pick_product(int M, int64_t n, int64_t kb) {
+  int best = best_tile(M, n, kb);
   for (int few = 3; M <= kFewRows && few < 6; ++few)
     if (kernel_us(few, M, n, kb) < kernel_us(best, M, n, kb)) best = few;
   return best;
@@ -485,17 +496,18 @@ static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st)
   return hipGetLastError();
 }
 
-// part: room for splits * M * N sums
+// part: room for splits * M * N sums.  terms: rows m, m + M / terms, ... are added, too.
 template <class E, class Epi>
-static hipError_t launch_split(const RowsProduct& p, const Epi& e, Split sp, void* part, hipStream_t st) {
+static hipError_t launch_split(const RowsProduct& p, const Epi& e, Split sp, void* part, hipStream_t st, int terms = 1) {
   typedef typename E::Sum S;
   const PartEpi<S> pe{static_cast<S*>(part), (int64_t)p.M * p.N, p.N, (p.N & 3) == 0};
   hipError_t err = sp.tile == 0   ? launch_rows<E, Rows256>(p, pe, st, sp.splits)
                    : sp.tile == 1 ? launch_rows<E, Rows128>(p, pe, st, sp.splits)
                                   : launch_rows<E, Rows64>(p, pe, st, sp.splits);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((finish_kernel<S, Epi>), grid_of(ceil_div((int64_t)p.M * p.N, 256)), dim3(256), 0, st, pe.out, pe.part_stride, sp.splits,
-                     p.M, p.rows_used, e);
+  const int rows = p.M / terms;
+  hipLaunchKernelGGL((finish_kernel<S, Epi>), grid_of(ceil_div((int64_t)rows * p.N, 256)), dim3(256), 0, st, pe.out, (int64_t)rows * p.N,
+                     sp.splits * terms, rows, p.rows_used, e);
   return hipGetLastError();
 }
 
@@ -638,13 +650,17 @@ asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely) {
   return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st, likely) : run_gated<ElemF16, _Float16>(p, o, st, likely);
 }
 
-// Gradient.  g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
+// Gradient.  Up to 64 rows, where the products are bound by the weights' bytes, dg and du enter the products as the sum of two
+// numbers each: rounded once, the few errors there are do not average out (4 rows of 136 channels: 1.5 times a rounded result's own
+// error instead of 1.0).
+// g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
 // over an index that is not the operands' rows' own (channels, rows), so their operands are transposed first, in passes that
 // cost a twentieth of the products at training sizes.
 struct GatedGradPlan {
   GatedPlan in;
   int Np;        // channels, padded to whole stages of k
   int64_t Mp;    // rows, likewise
+  int terms;     // numbers of `type` that stand for one of dg, du
   uint8_t *dgu, *dgu_t, *w_t, *x_t;
   Split dx, dw;
   uint8_t* part;   // partial sums of the one product, then of the other
@@ -656,13 +672,17 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   r.in = plan_gated(p, &c);
   r.Np = (int)(ceil_div(p.channels, 64) * 64);
   r.Mp = ceil_div(p.rows, 64) * 64;
-  r.dgu = c.take((size_t)2 * p.rows * 2 * r.Np);
+  r.terms = p.rows <= kFewRows ? 2 : 1;
+  const int64_t rows = (int64_t)r.terms * p.rows, Kp = r.terms * r.Mp;
+  r.dgu = c.take((size_t)2 * rows * 2 * r.Np);
   r.w_t = p.dx ? c.take((size_t)2 * p.cols * 2 * r.Np) : nullptr;
-  r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * r.Mp) : nullptr;
-  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * r.Mp) : nullptr;
-  r.dx = p.dx ? pick_split(p.rows, p.cols, 4 * (int64_t)r.Np) : Split{1, 0};
-  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, 2 * r.Mp) : Split{1, 0};
-  const size_t dx_sums = r.dx.splits > 1 ? (size_t)r.dx.splits * p.rows * p.cols : 0, dw_sums = r.dw.splits > 1 ? (size_t)r.dw.splits * 2 * r.Np * p.cols : 0;
+  r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * Kp) : nullptr;
+  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * Kp) : nullptr;
+  r.dx = p.dx ? pick_split((int)rows, p.cols, 4 * (int64_t)r.Np) : Split{1, 0};
+  if (r.dx.splits == 1) r.dx.tile = best_tile((int)rows, p.cols, 4 * (int64_t)r.Np);
+  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, 2 * Kp) : Split{1, 0};
+  const size_t dx_sums = p.dx && (r.dx.splits > 1 || r.terms > 1) ? (size_t)r.dx.splits * rows * p.cols : 0,
+               dw_sums = r.dw.splits > 1 ? (size_t)r.dw.splits * 2 * r.Np * p.cols : 0;
   r.part = c.take(sizeof(float) * std::max(dx_sums, dw_sums));
   r.bytes = c.used;
   return r;
@@ -693,22 +713,29 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   const GatedGradPlan o = plan_gated_grad(p);
   ASD_HIP(bring({&o.in.x, &o.in.g, &o.in.u}, st));
   T* dgu = reinterpret_cast<T*>(o.dgu);
-  const bool few = pick_product(p.rows, 2 * (int64_t)p.channels, k_bytes(2 * (int64_t)p.cols)) >= 3;   // (that kernel transposes nothing)
+  const int Np2 = 2 * o.Np;
+  const bool few = o.terms > 1;
+  const int64_t Kp = o.terms * o.Mp;
   const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act,
-                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
-  ASD_HIP(launch_product<E>(gated_product(p, o.in), e, st));
-  const Transpose16 gate = transposed(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, 2 * o.Np),
-                    up = transposed(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t ? o.w_t + 2 * (size_t)o.Np : nullptr, 2 * o.Np),
-                    x = transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t, o.Mp);
-  ASD_HIP(!p.dw_gate ? transpose16({gate, up}, st) : !p.dx ? transpose16({x}, st) : transpose16({gate, up, x}, st));
+                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, dgu + (int64_t)p.rows * Np2,
+                          few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
+  const RowsProduct first = gated_product(p, o.in);
+  if (few) ASD_HIP(p.rows <= 16 ? launch_few<E, 1>(first, e, st) : p.rows <= 32 ? launch_few<E, 2>(first, e, st) : launch_few<E, 4>(first, e, st));
+  else ASD_HIP(launch_product<E>(first, e, st));
   if (p.dx) {
-    const RowsProduct g{o.dgu, o.w_t, nullptr, 4 * (int64_t)o.Np, 4 * (int64_t)o.Np, 0, p.rows, p.cols, 4 * (int64_t)o.Np, nullptr};
+    ASD_HIP(transpose16({transposed(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, Np2),
+                         transposed(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2)}, st));
+    const RowsProduct g{o.dgu, o.w_t, nullptr, 2 * (int64_t)Np2, 2 * (int64_t)Np2, 0, o.terms * p.rows, p.cols, 2 * (int64_t)Np2, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
-    ASD_HIP(o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st) : launch_product<E>(g, s, st));
+    ASD_HIP(few || o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st, o.terms) : launch_product<E>(g, s, st));
   }
   if (p.dw_gate) {
-    if (few) ASD_HIP(transpose16({transposed(o.dgu, 2 * o.Np, p.rows, 2 * o.Np, o.dgu_t, o.Mp)}, st));
-    const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * o.Mp, 2 * o.Mp, 0, 2 * o.Np, p.cols, 2 * o.Mp, nullptr};
+    const Transpose16 x = transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t, Kp);
+    if (few)
+      ASD_HIP(transpose16({x, transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t + 2 * o.Mp, Kp), transposed(dgu, Np2, p.rows, Np2, o.dgu_t, Kp),
+                           transposed(e.lo, Np2, p.rows, Np2, o.dgu_t + 2 * o.Mp, Kp)}, st));
+    else ASD_HIP(transpose16({x}, st));
+    const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * Kp, 2 * Kp, 0, Np2, p.cols, 2 * Kp, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
                       on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
     ASD_HIP(o.dw.splits > 1 ? launch_split<E>(g, s, o.dw, o.part, st) : launch_product<E>(g, s, st));
