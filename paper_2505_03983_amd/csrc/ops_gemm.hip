@@ -240,7 +240,7 @@ struct GatedGradEpi {
   int64_t ld_dh;
   int N, act;
   bool dh_wide;   // runs of four of dh lie on 8 bytes
-  T* lo;          // (few rows) what the rounding of dgu leaves, rounded
+  T* lo;          // (kernel for few rows) what the rounding of dgu leaves, rounded
   T* turned;      // NULL, or the same transposed: [2 Np][Mp], zeros in the columns M .. Mp - 1
   int64_t Mp;
   __device__ __forceinline__ int turned_rows(int M) const { return turned ? (int)Mp : M; }
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * kCopyRows) void pack_rows_kernel(RowsCopies al
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
-// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to four matrices a launch.
+// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to six matrices a launch.
 struct Transpose16 {
   const uint16_t* src;
   uint16_t* dst;
@@ -352,8 +352,8 @@ struct Transpose16 {
   bool wide;   // rows on 16 bytes
 };
 struct Transposes16 {
-  Transpose16 t[4];
-  int64_t first[4];   // its first workgroup
+  Transpose16 t[6];
+  int64_t first[6];   // its first workgroup
   int n;
 };
 __global__ __launch_bounds__(256) void transpose16_kernel(Transposes16 all) {
@@ -650,12 +650,15 @@ asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely) {
   return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st, likely) : run_gated<ElemF16, _Float16>(p, o, st, likely);
 }
 
-// Gradient.  Up to 64 rows, where the products are bound by the weights' bytes, dg and du enter the products as the sum of two
-// numbers each: rounded once, the few errors there are do not average out (4 rows of 136 channels: 1.5 times a rounded result's own
-// error instead of 1.0).
+// Gradient.  dg and du enter the products rounded to the operands' type, which makes an error of the same size as the results' own
+// rounding: together 1.41 of it.  That is an average over rows times channels, or over the results, a few of which carry most of it:
+// where they are few, it came to 1.6 and more (65 rows of 64 channels: 1.8; 2100 rows, 64 channels of 64: 1.65).  There, and up to 64
+// rows, where the products are bound by the weights' bytes, each of them is the sum of two such numbers, formed by the kernel for few
+// rows.
 // g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
 // over an index that is not the operands' rows' own (channels, rows), so their operands are transposed first, in passes that
 // cost a twentieth of the products at training sizes.
+constexpr int64_t kFewNumbers = 1 << 17;
 struct GatedGradPlan {
   GatedPlan in;
   int Np;        // channels, padded to whole stages of k
@@ -672,7 +675,7 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   r.in = plan_gated(p, &c);
   r.Np = (int)(ceil_div(p.channels, 64) * 64);
   r.Mp = ceil_div(p.rows, 64) * 64;
-  r.terms = p.rows <= kFewRows ? 2 : 1;
+  r.terms = p.rows <= kFewRows || (int64_t)p.rows * p.channels <= kFewNumbers || (int64_t)p.channels * p.cols <= kFewNumbers ? 2 : 1;
   const int64_t rows = (int64_t)r.terms * p.rows, Kp = r.terms * r.Mp;
   r.dgu = c.take((size_t)2 * rows * 2 * r.Np);
   r.w_t = p.dx ? c.take((size_t)2 * p.cols * 2 * r.Np) : nullptr;
@@ -691,16 +694,10 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
 static Transpose16 transposed(const void* src, int64_t ld, int rows, int cols, uint8_t* dst, int64_t dst_ld) {
   return Transpose16{static_cast<const uint16_t*>(src), reinterpret_cast<uint16_t*>(dst), ld, dst_ld, rows, cols, on16(src, ld, 2)};
 }
-static hipError_t transpose16(std::initializer_list<Transpose16> list, hipStream_t st) {
-  Transposes16 all{};
-  int64_t grid = 0;
-  for (const Transpose16& t : list) {
-    all.first[all.n] = grid;
-    all.t[all.n++] = t;
-    grid += ceil_div(t.cols, 64) * ceil_div(t.rows, 64);
-  }
-  hipLaunchKernelGGL(transpose16_kernel, grid_of(grid), dim3(256), 0, st, all);
-  return hipGetLastError();
+static void add(Transposes16* all, int64_t* grid, const Transpose16& t) {
+  all->first[all->n] = *grid;
+  all->t[all->n++] = t;
+  *grid += ceil_div(t.cols, 64) * ceil_div(t.rows, 64);
 }
 
 __global__ __launch_bounds__(256) void zero16_kernel(uint16_t* p, int64_t ld, int rows, int cols) {
@@ -720,21 +717,27 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
                           ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, dgu + (int64_t)p.rows * Np2,
                           few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
   const RowsProduct first = gated_product(p, o.in);
-  if (few) ASD_HIP(p.rows <= 16 ? launch_few<E, 1>(first, e, st) : p.rows <= 32 ? launch_few<E, 2>(first, e, st) : launch_few<E, 4>(first, e, st));
+  if (few)
+    ASD_HIP(p.rows <= 16 ? launch_few<E, 1>(first, e, st) : p.rows <= 32 ? launch_few<E, 2>(first, e, st) : launch_few<E, 4>(first, e, st));
   else ASD_HIP(launch_product<E>(first, e, st));
+  Transposes16 all{};
+  int64_t grid = 0;
   if (p.dx) {
-    ASD_HIP(transpose16({transposed(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, Np2),
-                         transposed(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2)}, st));
+    add(&all, &grid, transposed(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, Np2));
+    add(&all, &grid, transposed(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2));
+  }
+  for (int t = 0; p.dw_gate && t < o.terms; ++t) {
+    add(&all, &grid, transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t + 2 * t * o.Mp, Kp));
+    if (few) add(&all, &grid, transposed(t ? e.lo : dgu, Np2, p.rows, Np2, o.dgu_t + 2 * t * o.Mp, Kp));
+  }
+  hipLaunchKernelGGL(transpose16_kernel, grid_of(grid), dim3(256), 0, st, all);
+  ASD_HIP(hipGetLastError());
+  if (p.dx) {
     const RowsProduct g{o.dgu, o.w_t, nullptr, 2 * (int64_t)Np2, 2 * (int64_t)Np2, 0, o.terms * p.rows, p.cols, 2 * (int64_t)Np2, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
     ASD_HIP(few || o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st, o.terms) : launch_product<E>(g, s, st));
   }
   if (p.dw_gate) {
-    const Transpose16 x = transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t, Kp);
-    if (few)
-      ASD_HIP(transpose16({x, transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t + 2 * o.Mp, Kp), transposed(dgu, Np2, p.rows, Np2, o.dgu_t, Kp),
-                           transposed(e.lo, Np2, p.rows, Np2, o.dgu_t + 2 * o.Mp, Kp)}, st));
-    else ASD_HIP(transpose16({x}, st));
     const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * Kp, 2 * Kp, 0, Np2, p.cols, 2 * Kp, nullptr};
     const SumEpi<T> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
                       on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};

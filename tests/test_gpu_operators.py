@@ -284,7 +284,8 @@ def test_gated_of_integers(rows, cols, channels, t, act):
 
 @pytest.mark.parametrize("rows, cols, channels", [(1, 1, 1), (2, 16, 64), (5, 7, 9), (64, 64, 64), (65, 130, 67), (100, 1000, 300),
                                                   (200, 72, 129), (130, 520, 1030), (1000, 256, 512), (700, 1100, 1500),
-                                                  (5000, 100, 140), (20, 72, 6000), (9001, 640, 72), (16, 33, 47)])
+                                                  (5000, 100, 140), (20, 72, 6000), (9001, 640, 72), (16, 33, 47), (300, 1001, 700),
+                                                  (2100, 300, 500)])
 @pytest.mark.parametrize("t, act", [(BF16, "silu"), (F16, "gelu")])
 def test_gated_gradient(rows, cols, channels, t, act):
     g = gen(rows + cols)
