@@ -720,14 +720,14 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   if (few)
     ASD_HIP(p.rows <= 16 ? launch_few<E, 1>(first, e, st) : p.rows <= 32 ? launch_few<E, 2>(first, e, st) : launch_few<E, 4>(first, e, st));
   else ASD_HIP(launch_product<E>(first, e, st));
-  Transposes16 all{};
+  Transposes16 all{};   // (of copies, where there are any: their rows are on 16 bytes)
   int64_t grid = 0;
   if (p.dx) {
-    add(&all, &grid, transposed(p.w_gate, p.ld_w_gate, p.channels, p.cols, o.w_t, Np2));
-    add(&all, &grid, transposed(p.w_up, p.ld_w_up, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2));
+    add(&all, &grid, transposed(o.in.g.p, o.in.g.pitch / 2, p.channels, p.cols, o.w_t, Np2));
+    add(&all, &grid, transposed(o.in.u.p, o.in.u.pitch / 2, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2));
   }
   for (int t = 0; p.dw_gate && t < o.terms; ++t) {
-    add(&all, &grid, transposed(p.x, p.ld_x, p.rows, p.cols, o.x_t + 2 * t * o.Mp, Kp));
+    add(&all, &grid, transposed(o.in.x.p, o.in.x.pitch / 2, p.rows, p.cols, o.x_t + 2 * t * o.Mp, Kp));
     if (few) add(&all, &grid, transposed(t ? e.lo : dgu, Np2, p.rows, Np2, o.dgu_t + 2 * t * o.Mp, Kp));
   }
   hipLaunchKernelGGL(transpose16_kernel, grid_of(grid), dim3(256), 0, st, all);
