@@ -68,7 +68,14 @@ struct RowsProduct {
   int M, N;                              // rows; channels (of one weight matrix)
   int64_t kb;
   const int32_t* rows_used;              // DEV or NULL: rows to work on where the host knows a bound, M, only
+  // Epilogues with kWrap: k runs over sums of several products one behind the other.  From these bytes of k on (multiples of 128, and
+  // so is kb) an operand's row is read again from its start.
+  uint32_t x_wrap = ~0u, w_wrap = ~0u;
 };
+template <class Epi>
+__device__ __forceinline__ uint32_t wrapped(uint32_t k, uint32_t at) {
+  return Epi::kWrap && k >= at ? k - at : k;
+}
 
 // BM x BN workgroup tile (BN counts both matrices' channels in a gated product), WGM x WGN wavefronts, BKB bytes of k per stage.
 template <int BM_, int BN_, int WGM_, int WGN_, int BKB_, int STAGES_>
@@ -121,9 +128,13 @@ __device__ __forceinline__ bool rows_tile(int tiles_m, int tiles_n, int* tm, int
 }
 
 // LDS of a wavefront's transposed results, and of a kernel.
+template <class Cfg>
+constexpr int rows_turned() {   // rows that are turned at a time
+  return Cfg::WM < 64 ? Cfg::WM : 64;
+}
 template <class Cfg, class Epi>
 constexpr int rows_turned_bytes() {
-  return Epi::kTurned ? Epi::kOutputs * (Cfg::WN / 2) * Cfg::WM * 2 : 0;
+  return Epi::kTurned ? Epi::kOutputs * (Cfg::WN / 2) * rows_turned<Cfg>() * 2 : 0;
 }
 template <class Cfg, class Epi, int B>
 constexpr int rows_lds_bytes() {
@@ -150,9 +161,10 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
   static_assert(SL >= 2 && SL <= 64 && (SL & (SL - 1)) == 0, "slots of a parked row");
   constexpr int FACTOR = GATED ? 32 / B : 0;                // blocks from a gate's to the matching up's
   uint8_t* park = lds + wave * (B * ROWB);
-  // the transposed copy, in 16-bit numbers: the wavefront's columns, WM rows each, behind the parked rows of all wavefronts; chunks of
+  // the transposed copy, in 16-bit numbers: the wavefront's columns, TURN rows each, behind the parked rows of all wavefronts; chunks of
   // eight rows are permuted by the column for the banks
-  constexpr int CH = Cfg::WM / 8;
+  constexpr int TURN = rows_turned<Cfg>(), CH = TURN / 8;
+  static_assert(!Epi::kTurned || (OB == 2 && TURN % B == 0 && CH >= 4), "16-bit numbers, whole blocks");
   uint8_t* turned = lds + NW * (B * ROWB) + wave * rows_turned_bytes<Cfg, Epi>();
   auto turned_key = [](int col) { return (col >> 2) * 2 & (CH - 1); };
   const int col0 = n0 + wn * COLS;                          // channel of the wavefront's first column
@@ -205,8 +217,8 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
             if (epi.turned) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const int col = o * COLS + c + r, at = i * B + lrow;
-                *reinterpret_cast<Out*>(turned + col * (Cfg::WM * 2) + (((at >> 3) ^ turned_key(col)) * 16) + (at & 7) * 2) =
+                const int col = o * COLS + c + r, at = i * B % TURN + lrow;
+                *reinterpret_cast<Out*>(turned + col * (TURN * 2) + (((at >> 3) ^ turned_key(col)) * 16) + (at & 7) * 2) =
                     mrow + lrow < M ? v[o][r] : (Out)0.f;
               }
             }
@@ -233,32 +245,36 @@ __device__ __forceinline__ void rows_epilogue(const Epi& epi, Acc (&acc)[NB][MB]
       const uint4 v = *reinterpret_cast<const uint4*>(park + r * ROWB + ((sl ^ (r & (SL - 1))) * 16));
       if (lane < RPI * SL && mrow + r < M) epi.store(sl / (SL / OUTS), mrow + r, col0 + sl % (SL / OUTS) * (16 / OB), v);
     }
-  }
-  if constexpr (Epi::kTurned) {
-    static_assert(OB == 2, "16-bit numbers");
-    if (epi.turned)
+    if constexpr (Epi::kTurned) {   // (rows end, for the transposed copy, at a multiple of 64: no block is left over)
+      if (epi.turned && (i + 1) * B % TURN == 0)
 #pragma unroll 4
-      for (int e = lane; e < OUTS * COLS * CH; e += 64) {
-        const int col = e / CH, ch = e % CH;
-        const uint4 v = *reinterpret_cast<const uint4*>(turned + col * (Cfg::WM * 2) + ((ch ^ turned_key(col)) * 16));
-        epi.store_turned(col / COLS, m0 + wm * Cfg::WM + ch * 8, col0 + col % COLS, M, v);
-      }
+        for (int e = lane; e < OUTS * COLS * CH; e += 64) {
+          const int col = e / CH, ch = e % CH;
+          const uint4 v = *reinterpret_cast<const uint4*>(turned + col * (TURN * 2) + ((ch ^ turned_key(col)) * 16));
+          epi.store_turned(col / COLS, mrow + B - TURN + ch * 8, col0 + col % COLS, v);
+        }
+    }
   }
 }
 
-// The share of k of a launch that splits it (gridDim.y workgroups a tile): whole stages, the last one takes what is left.
-__device__ __forceinline__ void take_share(RowsProduct& p) {
+// The share of k of a launch that splits it (gridDim.y workgroups a tile): whole stages, the last one takes what is left.  Returned:
+// what is to be added to k, where operands wrap; the operands start there otherwise.
+template <bool WRAP>
+__device__ __forceinline__ uint32_t take_share(RowsProduct& p) {
   const int64_t share = (p.kb + 128 * (int64_t)gridDim.y - 1) / (128 * (int64_t)gridDim.y) * 128, from = min(share * blockIdx.y, p.kb);
+  p.kb = min(share, p.kb - from);
+  if (WRAP) return (uint32_t)from;
   p.x += from;
   p.w0 += from;
-  p.kb = min(share, p.kb - from);
+  return 0;
 }
 
 template <class E, class Cfg, class Epi>
 __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
   constexpr bool GATED = Epi::kGated;
+  uint32_t k_base = 0;
   if constexpr (Epi::kSplit) {
-    take_share(p);
+    k_base = take_share<Epi::kWrap>(p);
     epi.out += blockIdx.y * epi.part_stride;
   }
   constexpr int BM = Cfg::BM, BN = Cfg::BN, MI = Cfg::MI, NJ = Cfg::NJ, BKB = Cfg::BKB, STAGES = Cfg::STAGES, NG = Cfg::NG;
@@ -303,16 +319,16 @@ __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, 
   auto second = [&](int i) { return GATED && (((wave + NW * i) * RPL >> 5) & 1); };   // the wavefront's load i is of w1
 
   // k runs over whole stages; what is left of it over BKB comes first, through registers and filled with zeros.
-  const int rest = (int)(p.kb % BKB), nk = (int)(p.kb / BKB) + (rest ? 1 : 0);
+  const int rest = Epi::kWrap ? 0 : (int)(p.kb % BKB), nk = (int)(p.kb / BKB) + (rest ? 1 : 0);
   const uint32_t k_first = rest ? (uint32_t)rest : 0u;   // the first stage that is loaded directly starts here: stage s at
-  auto k_of = [&](int s) { return (uint32_t)(rest ? (s - 1) * BKB + (int)k_first : s * BKB); };
+  auto k_of = [&](int s) { return k_base + (uint32_t)(rest ? (s - 1) * BKB + (int)k_first : s * BKB); };
   auto issue = [&](int s, uint8_t* sb, int first, int count) {
-    const uint32_t k = k_of(s);
+    const uint32_t k = k_of(s), kx = wrapped<Epi>(k, p.x_wrap), kw = wrapped<Epi>(k, p.w_wrap);
 #pragma unroll
     for (int q = 0; q < LPS; ++q) {
       if (q < first || q >= first + count) continue;
-      if (q < X_LOADS) load_rows_to_lds(xr, x_off[q], k, sb + (wave + NW * q) * 1024);
-      else load_rows_to_lds(second(q - X_LOADS) ? w1r : w0r, w_off[q - X_LOADS], k, sb + BM * BKB + (wave + NW * (q - X_LOADS)) * 1024);
+      if (q < X_LOADS) load_rows_to_lds(xr, x_off[q], kx, sb + (wave + NW * q) * 1024);
+      else load_rows_to_lds(second(q - X_LOADS) ? w1r : w0r, w_off[q - X_LOADS], kw, sb + BM * BKB + (wave + NW * (q - X_LOADS)) * 1024);
     }
   };
 
@@ -437,8 +453,9 @@ template <class E, class Epi>
 __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int tiles_m, int tiles_n, Epi epi) {
   typedef Rows256 Cfg;
   constexpr bool GATED = Epi::kGated;
+  uint32_t k_base = 0;
   if constexpr (Epi::kSplit) {
-    take_share(p);
+    k_base = take_share<Epi::kWrap>(p);
     epi.out += blockIdx.y * epi.part_stride;
   }
   constexpr int BM = 256, BKB = 128;
@@ -474,15 +491,15 @@ __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int t
       const int ch = GATED ? (wrow >> 6) * 32 + (wrow & 31) : wrow;
       w_off[h][q] = (uint32_t)((int64_t)min(ch, p.N - 1 - n0) * (GATED && h ? p.w_pitch1 : p.w_pitch0)) + wchunk;
     }
-  const int rest = (int)(p.kb % BKB), nk = (int)(p.kb / BKB) + (rest ? 1 : 0);
-  auto k_of = [&](int s) { return (uint32_t)(rest ? (s - 1) * BKB + rest : s * BKB); };
+  const int rest = Epi::kWrap ? 0 : (int)(p.kb % BKB), nk = (int)(p.kb / BKB) + (rest ? 1 : 0);
+  auto k_of = [&](int s) { return k_base + (uint32_t)(rest ? (s - 1) * BKB + rest : s * BKB); };
   auto issue = [&](int s, int h) {
-    const uint32_t k = k_of(s);
+    const uint32_t k = k_of(s), kx = wrapped<Epi>(k, p.x_wrap), kw = wrapped<Epi>(k, p.w_wrap);
     uint8_t* sb = rows_lds + (s & 1) * Cfg::STAGE_BYTES;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) load_rows_to_lds(xr, x_off[h][q], k, sb + x_blk[h][q] * 1024);
+    for (int q = 0; q < 2; ++q) load_rows_to_lds(xr, x_off[h][q], kx, sb + x_blk[h][q] * 1024);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) load_rows_to_lds(h ? w1r : w0r, w_off[h][q], k, sb + w_blk[h][q] * 1024);
+    for (int q = 0; q < 2; ++q) load_rows_to_lds(h ? w1r : w0r, w_off[h][q], kw, sb + w_blk[h][q] * 1024);
   };
 
   typename E::Acc16 acc[4][8];
@@ -635,10 +652,11 @@ __global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi e
       for (int h = 0; h < 2; ++h) {
         const int64_t k = k0 + (int64_t)s * NWAVES * 128 + h * 64 + quarter * 16;
         const bool in = k < p.kb;
+        const int64_t kx = Epi::kWrap && k >= p.x_wrap ? k - p.x_wrap : k, kw = Epi::kWrap && k >= p.w_wrap ? k - p.w_wrap : k;
 #pragma unroll
-        for (int t = 0; t < WT; ++t) wf[s][h][t] = in ? *reinterpret_cast<const v4i_b*>(wrow[t] + k) : zero;
+        for (int t = 0; t < WT; ++t) wf[s][h][t] = in ? *reinterpret_cast<const v4i_b*>(wrow[t] + kw) : zero;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xf[s][h][i] = in && there[i] ? *reinterpret_cast<const v4i_b*>(xrow[i] + k) : zero;
+        for (int i = 0; i < MT; ++i) xf[s][h][i] = in && there[i] ? *reinterpret_cast<const v4i_b*>(xrow[i] + kx) : zero;
       }
 #pragma unroll
     for (int s = 0; s < DEPTH; ++s)

@@ -28,7 +28,7 @@ __device__ __forceinline__ void store_cols(T* row, int n, int n_cols, uint4 v) {
 }
 
 // out = sum (a gradient's product); rows from `second` on go to the other output (dw_gate, dw_up as one product)
-template <class T>
+template <class T, bool WRAP = false>
 struct SumEpi {
   T* out;
   T* out2;
@@ -37,7 +37,7 @@ struct SumEpi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = false, kSplit = false, kTurned = false;
+  static constexpr bool kGated = false, kSplit = false, kTurned = false, kWrap = WRAP;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -65,7 +65,7 @@ struct SumEpi {
 };
 
 // Partial sums of a launch that splits k: part [split][rows][N] (S: float or int), added up in order by finish_kernel.
-template <class S>
+template <class S, bool WRAP>
 struct PartEpi {
   S* out;
   int64_t part_stride;
@@ -73,7 +73,7 @@ struct PartEpi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef S Out;
-  static constexpr bool kGated = false, kSplit = true, kTurned = false;
+  static constexpr bool kGated = false, kSplit = true, kTurned = false, kWrap = WRAP;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -113,7 +113,7 @@ struct Scaled8Epi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = false, kSplit = false, kTurned = false;
+  static constexpr bool kGated = false, kSplit = false, kTurned = false, kWrap = false;
   static constexpr int kOutputs = 1;
   struct Cols {
     float s[4], b[4];
@@ -168,7 +168,7 @@ struct GatedEpi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = true, kSplit = false, kTurned = false;
+  static constexpr bool kGated = true, kSplit = false, kTurned = false, kWrap = false;
   static constexpr int kOutputs = 1;
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
@@ -198,7 +198,7 @@ struct Gated8Epi {
   bool wide;
   __host__ __device__ __forceinline__ int columns() const { return N; }
   typedef T Out;
-  static constexpr bool kGated = true, kSplit = false, kTurned = false;
+  static constexpr bool kGated = true, kSplit = false, kTurned = false, kWrap = false;
   static constexpr int kOutputs = 1;
   struct Cols {
     float g[4], u[4];
@@ -229,9 +229,11 @@ struct Gated8Epi {
   __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(x_scale[m], gate_scale[n], up_scale[n], g, u); }
 };
 
-// dg = dh u act'(g) and du = dh act(g), side by side: dgu [rows][2 Np], zeros in the columns N .. Np - 1 of either half.  Rounded
-// to the operands' type, as the products that follow take them; the tiles store them transposed, too, for the one that contracts over
-// rows (as a pass of its own 230 us of 8192 x 2 * 16384, and a launch).
+// dg = dh u act'(g) and du = dh act(g), each as the sum of two numbers of the operands' type, what the products that follow take:
+// dgu [rows][2][2 Np] holds the numbers next to dg, du, then what their rounding leaves, rounded; zeros in the columns N .. Np - 1 of
+// every quarter.  (One number alone makes an error of the size of the results' own rounding: 1.41 of it together, and 1.8 over few
+// numbers.)  The tiles store them transposed, too, for the product that contracts over rows (as a pass of its own 230 us of 8192 x
+// 2 * 16384 numbers, and a launch).
 template <class T>
 struct GatedGradEpi {
   T* dgu;
@@ -240,17 +242,16 @@ struct GatedGradEpi {
   int64_t ld_dh;
   int N, act;
   bool dh_wide;   // runs of four of dh lie on 8 bytes
-  T* lo;          // (kernel for few rows) what the rounding of dgu leaves, rounded
-  T* turned;      // NULL, or the same transposed: [2 Np][Mp], zeros in the columns M .. Mp - 1
+  T* turned;      // NULL, or the same transposed: [2 Np][2][Mp], zeros in the columns M .. Mp - 1 of either half
   int64_t Mp;
   __device__ __forceinline__ int turned_rows(int M) const { return turned ? (int)Mp : M; }
-  __device__ __forceinline__ void store_turned(int which, int m, int n, int, uint4 v) const {
-    if (n < Np && m < Mp) *reinterpret_cast<uint4*>(turned + ((int64_t)which * Np + n) * Mp + m) = v;
+  __device__ __forceinline__ void store_turned(int which, int m, int n, uint4 v) const {
+    if (n < Np && m < Mp) *reinterpret_cast<uint4*>(turned + (((int64_t)(which & 1) * Np + n) * 2 + (which >> 1)) * Mp + m) = v;
   }
   __host__ __device__ __forceinline__ int columns() const { return Np; }
   typedef T Out;
-  static constexpr bool kGated = true, kSplit = false, kTurned = true;
-  static constexpr int kOutputs = 2;
+  static constexpr bool kGated = true, kSplit = false, kTurned = true, kWrap = false;
+  static constexpr int kOutputs = 4;   // dg, du, and what is left of them
   struct Row {};
   __device__ __forceinline__ Row row(int) const { return Row{}; }
   struct Cols {};
@@ -269,36 +270,38 @@ struct GatedGradEpi {
     }
     return x;
   }
-  __device__ __forceinline__ void values(Row, Cols, const Extra& x, int n, const float* g, const float* u, T (&v)[2][4]) const {
+  static __device__ __forceinline__ void split(float v, T* hi, T* lo) {
+    *hi = (T)v;
+    const float left = v - (float)*hi;
+    *lo = fabsf(left) < INFINITY ? (T)left : (T)0.f;   // (nothing is left of an infinity)
+  }
+  __device__ __forceinline__ void values(Row, Cols, const Extra& x, int n, const float* g, const float* u, T (&v)[4][4]) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float d = (float)x.dh[r];
       float value, slope;
       act_both(act, g[r], &value, &slope);
-      v[0][r] = n + r < N ? (T)(d * u[r] * slope) : (T)0.f;
-      v[1][r] = n + r < N ? (T)(d * value) : (T)0.f;
+      split(n + r < N ? d * u[r] * slope : 0.f, &v[0][r], &v[2][r]);
+      split(n + r < N ? d * value : 0.f, &v[1][r], &v[3][r]);
     }
   }
   static constexpr bool wide = true;
   __device__ __forceinline__ void store1(int, int, T) const {}
   __device__ __forceinline__ void one(int m, int n, float g, float u) const {
-    float value = 0.f, slope = 0.f, d = 0.f;
+    float dg = 0.f, du = 0.f;
     if (n < N) {
-      d = (float)dh[m * ld_dh + n];
+      const float d = (float)dh[m * ld_dh + n];
+      float value, slope;
       act_both(act, g, &value, &slope);
+      dg = d * u * slope;
+      du = d * value;
     }
-    const int64_t at = (int64_t)m * 2 * Np + n;
-    const float v[2] = {d * u * slope, d * value};
-#pragma unroll
-    for (int o = 0; o < 2; ++o) {
-      const T hi = n < N ? (T)v[o] : (T)0.f;
-      dgu[at + o * Np] = hi;
-      const float left = v[o] - (float)hi;
-      lo[at + o * Np] = n < N && fabsf(left) < INFINITY ? (T)left : (T)0.f;   // (nothing is left of an infinity)
-    }
+    T* at = dgu + (int64_t)m * 4 * Np + n;
+    split(dg, at, at + 2 * (int64_t)Np);
+    split(du, at + Np, at + 3 * (int64_t)Np);
   }
   __device__ __forceinline__ void store(int which, int m, int n, uint4 v) const {
-    if (n < Np) *reinterpret_cast<uint4*>(dgu + (int64_t)m * 2 * Np + which * Np + n) = v;
+    if (n < Np) *reinterpret_cast<uint4*>(dgu + ((int64_t)m * 4 + which) * Np + n) = v;
   }
 };
 
@@ -496,18 +499,17 @@ static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st)
   return hipGetLastError();
 }
 
-// part: room for splits * M * N sums.  terms: rows m, m + M / terms, ... are added, too.
+// part: room for splits * M * N sums.
 template <class E, class Epi>
-static hipError_t launch_split(const RowsProduct& p, const Epi& e, Split sp, void* part, hipStream_t st, int terms = 1) {
+static hipError_t launch_split(const RowsProduct& p, const Epi& e, Split sp, void* part, hipStream_t st) {
   typedef typename E::Sum S;
-  const PartEpi<S> pe{static_cast<S*>(part), (int64_t)p.M * p.N, p.N, (p.N & 3) == 0};
+  const PartEpi<S, Epi::kWrap> pe{static_cast<S*>(part), (int64_t)p.M * p.N, p.N, (p.N & 3) == 0};
   hipError_t err = sp.tile == 0   ? launch_rows<E, Rows256>(p, pe, st, sp.splits)
                    : sp.tile == 1 ? launch_rows<E, Rows128>(p, pe, st, sp.splits)
                                   : launch_rows<E, Rows64>(p, pe, st, sp.splits);
   if (err != hipSuccess) return err;
-  const int rows = p.M / terms;
-  hipLaunchKernelGGL((finish_kernel<S, Epi>), grid_of(ceil_div((int64_t)rows * p.N, 256)), dim3(256), 0, st, pe.out, (int64_t)rows * p.N,
-                     sp.splits * terms, rows, p.rows_used, e);
+  hipLaunchKernelGGL((finish_kernel<S, Epi>), grid_of(ceil_div((int64_t)p.M * p.N, 256)), dim3(256), 0, st, pe.out, pe.part_stride, sp.splits,
+                     p.M, p.rows_used, e);
   return hipGetLastError();
 }
 
@@ -650,20 +652,15 @@ asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely) {
   return p.type == ASD_BF16 ? run_gated<ElemBf16, __bf16>(p, o, st, likely) : run_gated<ElemF16, _Float16>(p, o, st, likely);
 }
 
-// Gradient.  dg and du enter the products rounded to the operands' type, which makes an error of the same size as the results' own
-// rounding: together 1.41 of it.  That is an average over rows times channels, or over the results, a few of which carry most of it:
-// where they are few, it came to 1.6 and more (65 rows of 64 channels: 1.8; 2100 rows, 64 channels of 64: 1.65).  There, and up to 64
-// rows, where the products are bound by the weights' bytes, each of them is the sum of two such numbers, formed by the kernel for few
-// rows.
-// g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
+// Gradient.  g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
 // over an index that is not the operands' rows' own (channels, rows), so their operands are transposed first, in passes that
-// cost a twentieth of the products at training sizes.
-constexpr int64_t kFewNumbers = 1 << 17;
+// cost a few hundredths of the products at training sizes.  dg and du enter as the sum of two numbers: k runs over the products of the
+// first ones and then of the second, against the same rows of the other operand.
 struct GatedGradPlan {
   GatedPlan in;
   int Np;        // channels, padded to whole stages of k
   int64_t Mp;    // rows, likewise
-  int terms;     // numbers of `type` that stand for one of dg, du
+  bool few;      // the kernel for few rows forms dg and du: nothing is stored transposed yet
   uint8_t *dgu, *dgu_t, *w_t, *x_t;
   Split dx, dw;
   uint8_t* part;   // partial sums of the one product, then of the other
@@ -675,16 +672,14 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   r.in = plan_gated(p, &c);
   r.Np = (int)(ceil_div(p.channels, 64) * 64);
   r.Mp = ceil_div(p.rows, 64) * 64;
-  r.terms = p.rows <= kFewRows || (int64_t)p.rows * p.channels <= kFewNumbers || (int64_t)p.channels * p.cols <= kFewNumbers ? 2 : 1;
-  const int64_t rows = (int64_t)r.terms * p.rows, Kp = r.terms * r.Mp;
-  r.dgu = c.take((size_t)2 * rows * 2 * r.Np);
+  r.few = pick_product(p.rows, 2 * (int64_t)p.channels, k_bytes((int64_t)p.cols * 2)) >= 3;
+  r.dgu = c.take((size_t)2 * p.rows * 4 * r.Np);
   r.w_t = p.dx ? c.take((size_t)2 * p.cols * 2 * r.Np) : nullptr;
-  r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * Kp) : nullptr;
-  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * Kp) : nullptr;
-  r.dx = p.dx ? pick_split((int)rows, p.cols, 4 * (int64_t)r.Np) : Split{1, 0};
-  if (r.dx.splits == 1) r.dx.tile = best_tile((int)rows, p.cols, 4 * (int64_t)r.Np);
-  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, 2 * Kp) : Split{1, 0};
-  const size_t dx_sums = p.dx && (r.dx.splits > 1 || r.terms > 1) ? (size_t)r.dx.splits * rows * p.cols : 0,
+  r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * 2 * r.Mp) : nullptr;
+  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * r.Mp) : nullptr;
+  r.dx = p.dx ? pick_split(p.rows, p.cols, 8 * (int64_t)r.Np) : Split{1, 0};
+  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, 4 * r.Mp) : Split{1, 0};
+  const size_t dx_sums = r.dx.splits > 1 ? (size_t)r.dx.splits * p.rows * p.cols : 0,
                dw_sums = r.dw.splits > 1 ? (size_t)r.dw.splits * 2 * r.Np * p.cols : 0;
   r.part = c.take(sizeof(float) * std::max(dx_sums, dw_sums));
   r.bytes = c.used;
@@ -711,36 +706,33 @@ static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   ASD_HIP(bring({&o.in.x, &o.in.g, &o.in.u}, st));
   T* dgu = reinterpret_cast<T*>(o.dgu);
   const int Np2 = 2 * o.Np;
-  const bool few = o.terms > 1;
-  const int64_t Kp = o.terms * o.Mp;
+  const int64_t Mp2 = 2 * o.Mp;
   const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act,
-                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, dgu + (int64_t)p.rows * Np2,
-                          few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
-  const RowsProduct first = gated_product(p, o.in);
-  if (few)
-    ASD_HIP(p.rows <= 16 ? launch_few<E, 1>(first, e, st) : p.rows <= 32 ? launch_few<E, 2>(first, e, st) : launch_few<E, 4>(first, e, st));
-  else ASD_HIP(launch_product<E>(first, e, st));
+                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, o.few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
+  ASD_HIP(launch_product<E>(gated_product(p, o.in), e, st));
   Transposes16 all{};   // (of copies, where there are any: their rows are on 16 bytes)
   int64_t grid = 0;
   if (p.dx) {
     add(&all, &grid, transposed(o.in.g.p, o.in.g.pitch / 2, p.channels, p.cols, o.w_t, Np2));
     add(&all, &grid, transposed(o.in.u.p, o.in.u.pitch / 2, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2));
   }
-  for (int t = 0; p.dw_gate && t < o.terms; ++t) {
-    add(&all, &grid, transposed(o.in.x.p, o.in.x.pitch / 2, p.rows, p.cols, o.x_t + 2 * t * o.Mp, Kp));
-    if (few) add(&all, &grid, transposed(t ? e.lo : dgu, Np2, p.rows, Np2, o.dgu_t + 2 * t * o.Mp, Kp));
+  if (p.dw_gate) {
+    add(&all, &grid, transposed(o.in.x.p, o.in.x.pitch / 2, p.rows, p.cols, o.x_t, o.Mp));
+    for (int t = 0; o.few && t < 2; ++t) add(&all, &grid, transposed(dgu + t * Np2, 2 * (int64_t)Np2, p.rows, Np2, o.dgu_t + 2 * t * o.Mp, Mp2));
   }
   hipLaunchKernelGGL(transpose16_kernel, grid_of(grid), dim3(256), 0, st, all);
   ASD_HIP(hipGetLastError());
   if (p.dx) {
-    const RowsProduct g{o.dgu, o.w_t, nullptr, 2 * (int64_t)Np2, 2 * (int64_t)Np2, 0, o.terms * p.rows, p.cols, 2 * (int64_t)Np2, nullptr};
-    const SumEpi<T> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
-    ASD_HIP(few || o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st, o.terms) : launch_product<E>(g, s, st));
+    RowsProduct g{o.dgu, o.w_t, nullptr, 4 * (int64_t)Np2, 2 * (int64_t)Np2, 0, p.rows, p.cols, 4 * (int64_t)Np2, nullptr};
+    g.w_wrap = 2 * (uint32_t)Np2;
+    const SumEpi<T, true> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
+    ASD_HIP(o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st) : launch_product<E>(g, s, st));
   }
   if (p.dw_gate) {
-    const RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * Kp, 2 * Kp, 0, Np2, p.cols, 2 * Kp, nullptr};
-    const SumEpi<T> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
-                      on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
+    RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * Mp2, Mp2, 0, Np2, p.cols, 2 * Mp2, nullptr};
+    g.w_wrap = (uint32_t)Mp2;
+    const SumEpi<T, true> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
+                            on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
     ASD_HIP(o.dw.splits > 1 ? launch_split<E>(g, s, o.dw, o.part, st) : launch_product<E>(g, s, st));
   }
   return ASD_OK;

@@ -148,3 +148,11 @@ def test_gated_network_refusals(kw, status):
     with pytest.raises(b.AsdError) as e:
         b.Ctx(s, den, 4, 2)
     assert e.value.status == status, b.last_error()
+
+
+def test_gated_gradient_workspace_of_a_tall_call():
+    """A million rows of 2048 through 64 channels: dg and du twice (as they lie and transposed, two numbers each) and x transposed;
+    nothing of rows times columns besides."""
+    n = L.asd_gated_ff_backward_workspace(C.byref(gated(rows=1 << 20, cols=2048, channels=64, ld_x=2048, ld_w_gate=2048, ld_w_up=2048,
+                                                        ld_dh=64, ld_dx=2048, ld_dw_gate=2048, ld_dw_up=2048)))
+    assert n <= (1 << 20) * 2 * (2048 + 2 * 4 * 64) + (64 << 20)
