@@ -229,27 +229,28 @@ struct Gated8Epi {
   __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(x_scale[m], gate_scale[n], up_scale[n], g, u); }
 };
 
-// dg = dh u act'(g) and du = dh act(g), each as the sum of two numbers of the operands' type, what the products that follow take:
-// dgu [rows][2][2 Np] holds the numbers next to dg, du, then what their rounding leaves, rounded; zeros in the columns N .. Np - 1 of
-// every quarter.  (One number alone makes an error of the size of the results' own rounding: 1.41 of it together, and 1.8 over few
-// numbers.)  The tiles store them transposed, too, for the product that contracts over rows (as a pass of its own 230 us of 8192 x
-// 2 * 16384 numbers, and a launch).
+// dg = dh u act'(g) and du = dh act(g), each as the sum of two bf16 numbers, what the products that follow take: dgu [rows][2][2 Np]
+// holds the numbers next to dg, du, then what their rounding leaves, rounded; zeros in the columns N .. Np - 1 of every quarter.  (One
+// number alone makes an error of the size of the results' own rounding: 1.41 of it together, and 1.8 over few numbers.  In fp16 dg and
+// du may also leave the type: a gradient of 1e-5 lies among its last bits, and dh u above 65504, where the sums are well inside.)
+// The tiles store them transposed, too, for the product that contracts over rows (as a pass of its own 230 us of 8192 x 2 * 16384
+// numbers, and a launch).
 template <class T>
 struct GatedGradEpi {
-  T* dgu;
+  __bf16* dgu;
   int Np;
   const T* dh;
   int64_t ld_dh;
   int N, act;
   bool dh_wide;   // runs of four of dh lie on 8 bytes
-  T* turned;      // NULL, or the same transposed: [2 Np][2][Mp], zeros in the columns M .. Mp - 1 of either half
+  __bf16* turned;      // NULL, or the same transposed: [2 Np][2][Mp], zeros in the columns M .. Mp - 1 of either half
   int64_t Mp;
   __device__ __forceinline__ int turned_rows(int M) const { return turned ? (int)Mp : M; }
   __device__ __forceinline__ void store_turned(int which, int m, int n, uint4 v) const {
     if (n < Np && m < Mp) *reinterpret_cast<uint4*>(turned + (((int64_t)(which & 1) * Np + n) * 2 + (which >> 1)) * Mp + m) = v;
   }
   __host__ __device__ __forceinline__ int columns() const { return Np; }
-  typedef T Out;
+  typedef __bf16 Out;
   static constexpr bool kGated = true, kSplit = false, kTurned = true, kWrap = false;
   static constexpr int kOutputs = 4;   // dg, du, and what is left of them
   struct Row {};
@@ -270,12 +271,12 @@ struct GatedGradEpi {
     }
     return x;
   }
-  static __device__ __forceinline__ void split(float v, T* hi, T* lo) {
-    *hi = (T)v;
+  static __device__ __forceinline__ void split(float v, __bf16* hi, __bf16* lo) {
+    *hi = (__bf16)v;
     const float left = v - (float)*hi;
-    *lo = fabsf(left) < INFINITY ? (T)left : (T)0.f;   // (nothing is left of an infinity)
+    *lo = fabsf(left) < INFINITY ? (__bf16)left : (__bf16)0.f;   // (nothing is left of an infinity)
   }
-  __device__ __forceinline__ void values(Row, Cols, const Extra& x, int n, const float* g, const float* u, T (&v)[4][4]) const {
+  __device__ __forceinline__ void values(Row, Cols, const Extra& x, int n, const float* g, const float* u, __bf16 (&v)[4][4]) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float d = (float)x.dh[r];
@@ -286,7 +287,7 @@ struct GatedGradEpi {
     }
   }
   static constexpr bool wide = true;
-  __device__ __forceinline__ void store1(int, int, T) const {}
+  __device__ __forceinline__ void store1(int, int, __bf16) const {}
   __device__ __forceinline__ void one(int m, int n, float g, float u) const {
     float dg = 0.f, du = 0.f;
     if (n < N) {
@@ -296,7 +297,7 @@ struct GatedGradEpi {
       dg = d * u * slope;
       du = d * value;
     }
-    T* at = dgu + (int64_t)m * 4 * Np + n;
+    __bf16* at = dgu + (int64_t)m * 4 * Np + n;
     split(dg, at, at + 2 * (int64_t)Np);
     split(du, at + Np, at + 3 * (int64_t)Np);
   }
@@ -346,11 +347,12 @@ __global__ __launch_bounds__(64 * kCopyRows) void pack_rows_kernel(RowsCopies al
 }
 
 // dst [cols][dst_ld] = src [rows][cols] transposed, 16-bit elements, 64 x 64 a workgroup; columns rows .. of dst up to the next
-// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to six matrices a launch.
+// multiple of 64 are zero (dst_ld and dst are multiples of 16 bytes and hold them).  Up to six matrices a launch.  lo > 0: src is fp16,
+// dst two bf16 numbers whose sum it is, the second `lo` elements behind the first (11 bits in 8 and what is left, 3).
 struct Transpose16 {
   const uint16_t* src;
   uint16_t* dst;
-  int64_t ld, dst_ld;
+  int64_t ld, dst_ld, lo;
   int rows, cols;
   bool wide;   // rows on 16 bytes
 };
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(256) void transpose16_kernel(Transposes16 all) {
   while (i + 1 < all.n && workgroup() >= all.first[i + 1]) ++i;
   const uint16_t* src = all.t[i].src;
   uint16_t* dst = all.t[i].dst;
-  const int64_t ld = all.t[i].ld, dst_ld = all.t[i].dst_ld;
+  const int64_t ld = all.t[i].ld, dst_ld = all.t[i].dst_ld, lo = all.t[i].lo;
   const int rows = all.t[i].rows, cols = all.t[i].cols;
   const bool wide = all.t[i].wide;
   const unsigned at = (unsigned)(workgroup() - all.first[i]), across = (unsigned)(cols + 63) / 64;
@@ -394,10 +396,22 @@ __global__ __launch_bounds__(256) void transpose16_kernel(Transposes16 all) {
   for (int pass = 0; pass < 2; ++pass) {
     const int c = pass * 32 + (t >> 3), r = (t & 7) * 8;
     if (c0 + c >= cols) continue;
-    uint32_t e[4] = {0u, 0u, 0u, 0u};
+    uint16_t* to = dst + (int64_t)(c0 + c) * dst_ld + r0 + r;
+    uint32_t e[4] = {0u, 0u, 0u, 0u}, left[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) e[k >> 1] |= (uint32_t)tile[r + k][c] << (16 * (k & 1));
-    *reinterpret_cast<uint4*>(dst + (int64_t)(c0 + c) * dst_ld + r0 + r) = make_uint4(e[0], e[1], e[2], e[3]);
+    for (int k = 0; k < 8; ++k) {
+      uint16_t v = tile[r + k][c];
+      if (lo) {
+        const float f = (float)__builtin_bit_cast(_Float16, v);
+        const __bf16 hi = (__bf16)f;
+        const float d = f - (float)hi;   // (nothing is left of an infinity or a NaN)
+        v = __builtin_bit_cast(uint16_t, hi);
+        left[k >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, fabsf(d) < INFINITY ? (__bf16)d : (__bf16)0.f) << (16 * (k & 1));
+      }
+      e[k >> 1] |= (uint32_t)v << (16 * (k & 1));
+    }
+    *reinterpret_cast<uint4*>(to) = make_uint4(e[0], e[1], e[2], e[3]);
+    if (lo) *reinterpret_cast<uint4*>(to + lo) = make_uint4(left[0], left[1], left[2], left[3]);
   }
 }
 
@@ -654,12 +668,14 @@ asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely) {
 
 // Gradient.  g and u are computed again in the kernel that forms dg and du from them and dh; both products that follow contract
 // over an index that is not the operands' rows' own (channels, rows), so their operands are transposed first, in passes that
-// cost a few hundredths of the products at training sizes.  dg and du enter as the sum of two numbers: k runs over the products of the
-// first ones and then of the second, against the same rows of the other operand.
+// cost a few hundredths of the products at training sizes.  dg and du enter as the sum of two bf16 numbers: k runs over the products of
+// the first ones and then of the second, against the same rows of the other operand; an fp16 operand is the sum of two as well, and
+// the first ones run over its second in a third pass (what is left out is 2^-16 of a product).
 struct GatedGradPlan {
   GatedPlan in;
   int Np;        // channels, padded to whole stages of k
   int64_t Mp;    // rows, likewise
+  int terms;     // numbers an operand transposed consists of
   bool few;      // the kernel for few rows forms dg and du: nothing is stored transposed yet
   uint8_t *dgu, *dgu_t, *w_t, *x_t;
   Split dx, dw;
@@ -673,12 +689,13 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   r.Np = (int)(ceil_div(p.channels, 64) * 64);
   r.Mp = ceil_div(p.rows, 64) * 64;
   r.few = pick_product(p.rows, 2 * (int64_t)p.channels, k_bytes((int64_t)p.cols * 2)) >= 3;
+  r.terms = p.type == ASD_F16 ? 2 : 1;
   r.dgu = c.take((size_t)2 * p.rows * 4 * r.Np);
-  r.w_t = p.dx ? c.take((size_t)2 * p.cols * 2 * r.Np) : nullptr;
+  r.w_t = p.dx ? c.take((size_t)2 * p.cols * r.terms * 2 * r.Np) : nullptr;
   r.dgu_t = p.dw_gate ? c.take((size_t)2 * 2 * r.Np * 2 * r.Mp) : nullptr;
-  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * r.Mp) : nullptr;
-  r.dx = p.dx ? pick_split(p.rows, p.cols, 8 * (int64_t)r.Np) : Split{1, 0};
-  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, 4 * r.Mp) : Split{1, 0};
+  r.x_t = p.dw_gate ? c.take((size_t)2 * p.cols * r.terms * r.Mp) : nullptr;
+  r.dx = p.dx ? pick_split(p.rows, p.cols, (r.terms + 1) * 4 * (int64_t)r.Np) : Split{1, 0};
+  r.dw = p.dw_gate ? pick_split(2 * r.Np, p.cols, (r.terms + 1) * 2 * r.Mp) : Split{1, 0};
   const size_t dx_sums = r.dx.splits > 1 ? (size_t)r.dx.splits * p.rows * p.cols : 0,
                dw_sums = r.dw.splits > 1 ? (size_t)r.dw.splits * 2 * r.Np * p.cols : 0;
   r.part = c.take(sizeof(float) * std::max(dx_sums, dw_sums));
@@ -686,8 +703,8 @@ static GatedGradPlan plan_gated_grad(const asd_gated& p) {
   return r;
 }
 
-static Transpose16 transposed(const void* src, int64_t ld, int rows, int cols, uint8_t* dst, int64_t dst_ld) {
-  return Transpose16{static_cast<const uint16_t*>(src), reinterpret_cast<uint16_t*>(dst), ld, dst_ld, rows, cols, on16(src, ld, 2)};
+static Transpose16 transposed(const void* src, int64_t ld, int rows, int cols, uint8_t* dst, int64_t dst_ld, int64_t lo) {
+  return Transpose16{static_cast<const uint16_t*>(src), reinterpret_cast<uint16_t*>(dst), ld, dst_ld, lo, rows, cols, on16(src, ld, 2)};
 }
 static void add(Transposes16* all, int64_t* grid, const Transpose16& t) {
   all->first[all->n] = *grid;
@@ -704,36 +721,42 @@ template <class E, class T>
 static asd_status run_gated_grad(const asd_gated& p, hipStream_t st) {
   const GatedGradPlan o = plan_gated_grad(p);
   ASD_HIP(bring({&o.in.x, &o.in.g, &o.in.u}, st));
-  T* dgu = reinterpret_cast<T*>(o.dgu);
+  __bf16 *dgu = reinterpret_cast<__bf16*>(o.dgu), *dgu_t = reinterpret_cast<__bf16*>(o.dgu_t);
   const int Np2 = 2 * o.Np;
-  const int64_t Mp2 = 2 * o.Mp;
   const GatedGradEpi<T> e{dgu, o.Np, static_cast<const T*>(p.dh), p.ld_dh, p.channels, p.act,
-                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, o.few ? nullptr : reinterpret_cast<T*>(o.dgu_t), o.Mp};
+                          ((uintptr_t)p.dh & 7) == 0 && (p.ld_dh & 3) == 0, o.few ? nullptr : dgu_t, o.Mp};
   ASD_HIP(launch_product<E>(gated_product(p, o.in), e, st));
   Transposes16 all{};   // (of copies, where there are any: their rows are on 16 bytes)
   int64_t grid = 0;
+  const int64_t w_ld = (int64_t)o.terms * Np2, x_ld = o.terms * o.Mp, w_lo = o.terms > 1 ? Np2 : 0, x_lo = o.terms > 1 ? o.Mp : 0;
   if (p.dx) {
-    add(&all, &grid, transposed(o.in.g.p, o.in.g.pitch / 2, p.channels, p.cols, o.w_t, Np2));
-    add(&all, &grid, transposed(o.in.u.p, o.in.u.pitch / 2, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, Np2));
+    add(&all, &grid, transposed(o.in.g.p, o.in.g.pitch / 2, p.channels, p.cols, o.w_t, w_ld, w_lo));
+    add(&all, &grid, transposed(o.in.u.p, o.in.u.pitch / 2, p.channels, p.cols, o.w_t + 2 * (size_t)o.Np, w_ld, w_lo));
   }
   if (p.dw_gate) {
-    add(&all, &grid, transposed(o.in.x.p, o.in.x.pitch / 2, p.rows, p.cols, o.x_t, o.Mp));
-    for (int t = 0; o.few && t < 2; ++t) add(&all, &grid, transposed(dgu + t * Np2, 2 * (int64_t)Np2, p.rows, Np2, o.dgu_t + 2 * t * o.Mp, Mp2));
+    add(&all, &grid, transposed(o.in.x.p, o.in.x.pitch / 2, p.rows, p.cols, o.x_t, x_ld, x_lo));
+    for (int t = 0; o.few && t < 2; ++t)
+      add(&all, &grid, transposed(dgu + t * Np2, 2 * (int64_t)Np2, p.rows, Np2, o.dgu_t + 2 * t * o.Mp, 2 * o.Mp, 0));
   }
   hipLaunchKernelGGL(transpose16_kernel, grid_of(grid), dim3(256), 0, st, all);
   ASD_HIP(hipGetLastError());
+  // bytes of k of one product: 2 Np2, or 2 Mp
+  const auto product = [&](const uint8_t* x, const uint8_t* w, int rows, int64_t kb) {
+    RowsProduct g{x, w, nullptr, 2 * kb, o.terms * kb, 0, rows, p.cols, (o.terms + 1) * kb, nullptr};
+    g.x_wrap = 2 * (uint32_t)kb;
+    g.w_wrap = (uint32_t)kb;
+    return g;
+  };
   if (p.dx) {
-    RowsProduct g{o.dgu, o.w_t, nullptr, 4 * (int64_t)Np2, 2 * (int64_t)Np2, 0, p.rows, p.cols, 4 * (int64_t)Np2, nullptr};
-    g.w_wrap = 2 * (uint32_t)Np2;
+    const RowsProduct g = product(o.dgu, o.w_t, p.rows, 2 * (int64_t)Np2);
     const SumEpi<T, true> s{static_cast<T*>(p.dx), nullptr, p.ld_dx, 0, p.cols, p.rows, p.rows, on16(p.dx, p.ld_dx, 2)};
-    ASD_HIP(o.dx.splits > 1 ? launch_split<E>(g, s, o.dx, o.part, st) : launch_product<E>(g, s, st));
+    ASD_HIP(o.dx.splits > 1 ? launch_split<ElemBf16>(g, s, o.dx, o.part, st) : launch_product<ElemBf16>(g, s, st));
   }
   if (p.dw_gate) {
-    RowsProduct g{o.dgu_t, o.x_t, nullptr, 2 * Mp2, Mp2, 0, Np2, p.cols, 2 * Mp2, nullptr};
-    g.w_wrap = (uint32_t)Mp2;
+    const RowsProduct g = product(o.dgu_t, o.x_t, Np2, 2 * o.Mp);
     const SumEpi<T, true> s{static_cast<T*>(p.dw_gate), static_cast<T*>(p.dw_up), p.ld_dw_gate, p.ld_dw_up, p.cols, p.channels, o.Np,
                             on16(p.dw_gate, p.ld_dw_gate, 2) && on16(p.dw_up, p.ld_dw_up, 2)};
-    ASD_HIP(o.dw.splits > 1 ? launch_split<E>(g, s, o.dw, o.part, st) : launch_product<E>(g, s, st));
+    ASD_HIP(o.dw.splits > 1 ? launch_split<ElemBf16>(g, s, o.dw, o.part, st) : launch_product<ElemBf16>(g, s, st));
   }
   return ASD_OK;
 }
