@@ -1,0 +1,62 @@
+"""The operators at the ends of their types' ranges and sizes, against their definitions in 64 bits.
+
+u = 2^-24 is half a step of fp32, `half` that of a result's type."""
+import pytest
+import torch
+
+from paper_2505_03983_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def O():
+    from paper_2505_03983_amd import operators
+    return operators
+
+
+def half(t):
+    return torch.finfo(t).eps / 2
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+# sizes of a row's numbers and of its dy: products of both leave fp32 above and below; dx, about dy / r, stays inside
+ROWS = [(1.0, 1.0), (2.0 ** 124, 10.0), (2.0 ** 121, 2.0 ** 30), (2.0 ** -100, 1.0), (2.0 ** -126, 2.0 ** -20), (2.0 ** -130, 2.0 ** -30),
+        (2.0 ** 60, 2.0 ** 90), (2.0 ** -70, 2.0 ** -90), (3.0, 2.0 ** 60)]
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("cols", [5, 600, 1032, 4104, 9000, 20001])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_norm_gradient_of_large_and_small_rows(cols, t, eps):
+    g = torch.Generator(device=DEV).manual_seed(cols)
+    size = torch.tensor(ROWS, dtype=torch.float64, device=DEV)
+    r = (randn(g, len(ROWS), cols).clamp(-4, 4).double() * size[:, :1]).to(t)
+    r[:, 0] = size[:, 0].to(t)         # (a row of few bits is not all zeros)
+    dy = (randn(g, len(ROWS), cols).double() * size[:, 1:]).to(t)
+    gain = (1 + 0.2 * randn(g, cols)).to(t)
+    # a row alone: its dgain is its own, whatever the others hold
+    for rows in [slice(i, i + 1) for i in range(len(ROWS))] + [slice(0, len(ROWS))]:
+        rr, yy = r[rows], dy[rows]
+        d, gd, dyd = rr.double(), gain.double(), yy.double()
+        rstd = 1.0 / torch.sqrt(d.square().mean(1, keepdim=True) + eps)
+        n = d * rstd
+        want = rstd * (gd * dyd - n * (gd * dyd * n).mean(1, keepdim=True))
+        dx, dgain = O().rms_norm_backward(yy, rr, gain, eps)
+        # roundings to fp32: gain dy (1); n, from 1 / |r| and a product (2); the mean, of sums in 64 bits (1); their product, the difference,
+        # and two for the product with 1 / |r|.  Then the type's
+        slack = 8 * U * rstd * ((gd * dyd).abs() + (n * (gd * dyd * n).mean(1, keepdim=True)).abs() + n.abs() * (gd * dyd * n).abs().mean(1, keepdim=True))
+        tol = half(t) * want.abs() + 2 * slack + float(torch.finfo(t).smallest_normal)
+        assert bool(torch.isfinite(dx).all()), ROWS[rows]
+        assert float(((dx.double() - want).abs() - tol).max()) <= 0.0, ROWS[rows]
+        # n to fp32, a product and a sum a row
+        terms = (dyd * n).abs().sum(0)
+        slack = (len(ROWS) + 4) * U * terms + float(torch.finfo(F32).smallest_normal)
+        want = (dyd * n).sum(0)
+        assert bool(torch.isfinite(dgain).all()), ROWS[rows]
+        assert float(((dgain.double() - want).abs() - slack - half(t) * (want.abs() + slack)).max()) <= 0.0, ROWS[rows]
