@@ -6,6 +6,10 @@
 // All element types share one geometry, counted in bytes of k: a matrix instruction takes 16 bytes a lane of each operand
 // (8 numbers of 16 bits, 16 integers of 8), 32 bytes of k for 32 rows, and runs for as many cycles with either.
 //
+// A result's bits do not depend on the tile: all tiles add 32 or 64 bytes of k at a time from its start on, what is left of k over whole
+// stages first, and the instructions of either shape add up what they take in the same order (as their results say, which the tests
+// compare).  The kernel for few rows adds in another order.
+//
 // The channels' fragment goes in as the instruction's first operand, the rows' as its second: a lane then holds four
 // neighbouring channels of one row in four neighbouring registers, which is what the epilogues store.
 //

@@ -597,7 +597,8 @@ uint32_t mlp_verify_tiles(const asd_ctx* ctx, int likely, int most) {
   if (s->gated) {
     const asd_gated_blocks& g = s->blocks;
     const int64_t e = g.type == ASD_I8 ? 1 : 2;
-    tiles = 64 * tiles + 8 * (uint32_t)product_pick(likely, 2 * (int64_t)g.hidden, e * s->width) + (uint32_t)product_pick(likely, s->width, e * g.hidden);
+    tiles = 64 * tiles + 8 * (uint32_t)product_pick(likely, most, 2 * (int64_t)g.hidden, e * s->width) +
+            (uint32_t)product_pick(likely, most, s->width, e * g.hidden);
   }
   return tiles;
 }

@@ -55,7 +55,7 @@ __device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gr
 // For the library's own launches: the operators without their argument checks.
 asd_status launch_rms_norm(const asd_norm& p, hipStream_t st);
 asd_status launch_quantize_rows(const asd_norm& p, hipStream_t st);
-// likely: rows to expect, where the device knows their number (0: all): which kernel suits, nothing else
+// likely: rows to expect, where the device knows their number (0: all): which tile suits, no bit of the results
 // split: the workspace has room for partial sums, where few tiles have long ones
 asd_status launch_linear8(const asd_linear8& p, hipStream_t st, bool split, int likely = 0);
 asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely = 0);
@@ -63,8 +63,8 @@ asd_status launch_gated(const asd_gated& p, hipStream_t st, int likely = 0);
 asd_status launch_linear_bf16(const void* x, const void* w, float* out, int rows, int cols, int channels, const int32_t* rows_used,
                               hipStream_t st, int likely);
 // Microseconds of a product of `rows` rows with `channels` channels (both matrices' of a gated one) of kb bytes, on the kernel picked
-// for `most` rows; and that kernel's number, below 8.
+// for `most` rows; and the number, below 8, of the kernel that a call of up to `most` rows takes where `rows` are likely.
 double product_us(int rows, int most, int64_t channels, int64_t kb);
-int product_pick(int rows, int64_t channels, int64_t kb);
+int product_pick(int rows, int most, int64_t channels, int64_t kb);
 
 }  // namespace asd

@@ -480,13 +480,20 @@ static int best_tile(int M, int64_t n, int64_t kb) {
     if (kernel_us(i, M, n, kb) < kernel_us(best, M, n, kb)) best = i;
   return best;
 }
-static int pick_product(int M, int64_t n, int64_t kb) {
-  int best = best_tile(M, n, kb);
-  for (int few = 3; M <= kFewRows && few < 6; ++few)
-    if (kernel_us(few, M, n, kb) < kernel_us(best, M, n, kb)) best = few;
+static int best_few(int M, int64_t n, int64_t kb) {
+  int best = 3;
+  for (int i = 4; i < 6; ++i)
+    if (kernel_us(i, M, n, kb) < kernel_us(best, M, n, kb)) best = i;
   return best;
 }
-int product_pick(int rows, int64_t channels, int64_t kb) { return pick_product(rows, channels, kb); }
+// likely: rows to expect of the M there may be.  They choose among the tiles, or among the forms of the kernel for few rows, which all
+// give a row the same bits; which of the two it is goes by M alone.
+static int pick_product(int M, int64_t n, int64_t kb, int likely) {
+  const int tile = best_tile(M, n, kb), few = best_few(M, n, kb);
+  return M <= kFewRows && kernel_us(few, M, n, kb) < kernel_us(tile, M, n, kb) ? best_few(likely, n, kb) : best_tile(likely, n, kb);
+}
+static int pick_product(int M, int64_t n, int64_t kb) { return pick_product(M, n, kb, M); }
+int product_pick(int rows, int most, int64_t channels, int64_t kb) { return pick_product(most, channels, kb, rows); }
 double product_us(int rows, int most, int64_t channels, int64_t kb) { return kernel_us(pick_product(most, channels, kb), rows, channels, kb); }
 
 // How a product whose caller has room for partial sums splits k: few tiles and long sums.  {1, 0}: not at all.
@@ -529,8 +536,7 @@ static hipError_t launch_split(const RowsProduct& p, const Epi& e, Split sp, voi
 
 template <class E, class Epi>
 static hipError_t launch_product(const RowsProduct& p, const Epi& e, hipStream_t st, int likely = 0) {
-  int pick = pick_product(likely > 0 ? std::min(likely, p.M) : p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb);
-  if (pick >= 3 && ceil_div(p.M, 16 << (pick - 3)) > 65535) pick = 2;   // (few are likely of very many: a dimension of the grid)
+  const int pick = pick_product(p.M, Epi::kGated ? 2 * (int64_t)p.N : p.N, p.kb, likely > 0 ? std::min(likely, p.M) : p.M);
   if (pick == 3) return launch_few<E, 1>(p, e, st);
   if (pick == 4) return launch_few<E, 2>(p, e, st);
   if (pick == 5) return launch_few<E, 4>(p, e, st);
