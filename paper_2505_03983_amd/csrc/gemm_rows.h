@@ -626,8 +626,9 @@ __global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi e
   constexpr bool GATED = Epi::kGated;
   constexpr int WT = GATED ? 2 : 1, NWAVES = 8, DEPTH = MT == 1 ? 4 : 2;
   const int M = p.rows_used ? min(max(*p.rows_used, 0), p.M) : p.M;
-  const int m0 = blockIdx.y * (16 * MT), n0 = blockIdx.x * 16;
-  if (m0 >= M) return;
+  // (channels over two dimensions of the grid: 2^28 of them are more than 2^32 threads)
+  const int m0 = blockIdx.z * (16 * MT), n0 = (int)(blockIdx.y * gridDim.x + blockIdx.x) * 16;
+  if (m0 >= M || n0 >= epi.columns()) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
   const uint8_t* wrow[WT];
   wrow[0] = p.w0 + (int64_t)min(n0 + l16, p.N - 1) * p.w_pitch0;

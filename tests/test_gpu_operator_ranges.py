@@ -60,3 +60,29 @@ def test_norm_gradient_of_large_and_small_rows(cols, t, eps):
         want = (dyd * n).sum(0)
         assert bool(torch.isfinite(dgain).all()), ROWS[rows]
         assert float(((dgain.double() - want).abs() - slack - half(t) * (want.abs() + slack)).max()) <= 0.0, ROWS[rows]
+
+
+def test_one_row_through_more_channels_than_threads_in_a_dimension():
+    """2^27 channels, 16 a workgroup of 512 threads: 2^32 threads and more."""
+    channels = (1 << 27) + 37
+    w = torch.zeros(channels, 16, dtype=torch.int8, device=DEV)
+    for at in (0, 17, 1 << 26, (1 << 27) - 1, 1 << 27, channels - 1):
+        w[at, 3] = at % 100 + 1
+    x = torch.ones(1, 16, dtype=torch.int8, device=DEV)
+    y = O().linear_i8(x, torch.ones(1, device=DEV), w, torch.ones(channels, device=DEV), out_type=F32)
+    assert torch.equal(y[0], w[:, 3].float())
+
+
+def test_norm_gradient_of_more_rows_than_threads_in_a_dimension():
+    """70 million rows of 8 in two sizes, each by its own, so that dgain is a count."""
+    rows = 70_000_000
+    r = torch.full((rows, 8), 2.0, dtype=F16, device=DEV)
+    r[::2] = -0.5
+    dy = torch.zeros(rows, 8, dtype=F16, device=DEV)
+    dy[-3:] = 1.0            # rows -2.0 / 2.0 apart from their signs: n = 1, -1, 1
+    dy[5] = 2.0
+    dx, dgain = O().rms_norm_backward(dy, r, eps=0.0)
+    signs = torch.where(r[:, 0] > 0, 1.0, -1.0)
+    want = float((signs.double() * dy[:, 0].double()).sum())
+    assert dgain.tolist() == [want] * 8
+    assert float(dx.float().abs().max()) == 0.0
