@@ -101,6 +101,15 @@ __global__ __launch_bounds__(256) void finish_kernel(const S* __restrict__ part,
   epi.one((int)m, (int)(at - m * N), s, s);
 }
 
+// A row's scale: s up.  A sum of 31 bits times a scale above 2^96 may leave fp32, where the channel's scale brings it back: such a scale
+// goes in as 2^-32 of itself, and 2^32 at the end.
+struct RowScale {
+  float s, up;
+};
+__device__ __forceinline__ RowScale row_scale(float v) {
+  return v > 0x1p96f ? RowScale{v * 0x1p-32f, 0x1p32f} : RowScale{v, 1.f};
+}
+
 // out = sum x_scale w_scale + bias
 template <class T>
 struct Scaled8Epi {
@@ -120,7 +129,7 @@ struct Scaled8Epi {
   };
   struct Extra {};
   __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
-  __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
+  __device__ __forceinline__ RowScale row(int m) const { return row_scale(x_scale[m]); }
   __device__ __forceinline__ Cols cols(int n) const {
     Cols c;
 #pragma unroll
@@ -130,15 +139,18 @@ struct Scaled8Epi {
     }
     return c;
   }
-  __device__ __forceinline__ void values(float xs, const Cols& c, Extra, int, const int* a, const int*, T (&v)[1][4]) const {
+  __device__ __forceinline__ void values(RowScale x, const Cols& c, Extra, int, const int* a, const int*, T (&v)[1][4]) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[0][r] = (T)((float)a[r] * xs * c.s[r] + c.b[r]);
+    for (int r = 0; r < 4; ++r) v[0][r] = (T)fmaf((float)a[r] * x.s * c.s[r], x.up, c.b[r]);
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
   __device__ __forceinline__ void store1(int m, int n, T v) const {
     if (n < N) out[m * ld + n] = v;
   }
-  __device__ __forceinline__ void one(int m, int n, int a, int) const { out[m * ld + n] = (T)((float)a * x_scale[m] * w_scale[n] + (bias ? bias[n] : 0.f)); }
+  __device__ __forceinline__ void one(int m, int n, int a, int) const {
+    const RowScale x = row(m);
+    out[m * ld + n] = (T)fmaf((float)a * x.s * w_scale[n], x.up, bias ? bias[n] : 0.f);
+  }
 };
 
 // Activations and their derivatives, in fp32.  exp2 and the reciprocal are the hardware's (1 ulp each): about 1e-6 of the value,
@@ -205,7 +217,7 @@ struct Gated8Epi {
   };
   struct Extra {};
   __device__ __forceinline__ Extra extra(int, int) const { return Extra{}; }
-  __device__ __forceinline__ float row(int m) const { return x_scale[m]; }
+  __device__ __forceinline__ RowScale row(int m) const { return row_scale(x_scale[m]); }
   __device__ __forceinline__ Cols cols(int n) const {
     Cols c;
 #pragma unroll
@@ -215,18 +227,18 @@ struct Gated8Epi {
     }
     return c;
   }
-  __device__ __forceinline__ T value(float xs, float gs, float us, int g, int u) const {
-    return (T)(act_value(act, (float)g * xs * gs) * ((float)u * xs * us));
+  __device__ __forceinline__ T value(RowScale x, float gs, float us, int g, int u) const {
+    return (T)(act_value(act, (float)g * x.s * gs * x.up) * ((float)u * x.s * us * x.up));
   }
-  __device__ __forceinline__ void values(float xs, const Cols& c, Extra, int, const int* g, const int* u, T (&v)[1][4]) const {
+  __device__ __forceinline__ void values(RowScale x, const Cols& c, Extra, int, const int* g, const int* u, T (&v)[1][4]) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[0][r] = value(xs, c.g[r], c.u[r], g[r], u[r]);
+    for (int r = 0; r < 4; ++r) v[0][r] = value(x, c.g[r], c.u[r], g[r], u[r]);
   }
   __device__ __forceinline__ void store(int, int m, int n, uint4 v) const { store_cols(out + m * ld, n, N, v); }
   __device__ __forceinline__ void store1(int m, int n, T v) const {
     if (n < N) out[m * ld + n] = v;
   }
-  __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(x_scale[m], gate_scale[n], up_scale[n], g, u); }
+  __device__ __forceinline__ void one(int m, int n, int g, int u) const { out[m * ld + n] = value(row(m), gate_scale[n], up_scale[n], g, u); }
 };
 
 // dg = dh u act'(g) and du = dh act(g), each as the sum of two bf16 numbers, what the products that follow take: dgu [rows][2][2 Np]

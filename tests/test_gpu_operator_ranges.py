@@ -86,3 +86,26 @@ def test_norm_gradient_of_more_rows_than_threads_in_a_dimension():
     want = float((signs.double() * dy[:, 0].double()).sum())
     assert dgain.tolist() == [want] * 8
     assert float(dx.float().abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("rows", [1, 40, 300, 2000])
+def test_products_of_rows_with_large_scales(rows):
+    """Rows next to fp32's largest number, weights as small as that: the sum times one scale leaves fp32, times both it does not."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    cols, channels = 272, 2100
+    q, qs = O().quantize_rows(randn(g, rows, cols).clamp(-3, 3) * 1e38)
+    w, ws = O().quantize_rows(randn(g, channels, cols) * 1e-36)
+    w2, ws2 = O().quantize_rows(randn(g, channels, cols) * 1e-36)
+    assert bool(torch.isfinite(qs).all()) and bool(torch.isinf((q.float() @ w.float().T).abs() * qs[:, None]).any())
+    product = lambda a, s: (q.double() @ a.double().T) * qs.double()[:, None] * s.double()   # noqa: E731
+    want = product(w, ws)
+    bias = randn(g, channels)
+    y = O().linear_i8(q, qs, w, ws, bias, F32)
+    # the sum as fp32, two scalings, the bias
+    assert float(((y.double() - want - bias.double()).abs() - 4 * U * (want.abs() + (want + bias.double()).abs())).max()) <= 0.0
+    zg, zu = want, product(w2, ws2)
+    want = zg * torch.sigmoid(zg) * zu
+    # |act'| <= 1.13; the activation to 2^-20 (1 + |z|) of itself, its sigmoid to fp32's smallest normal number
+    slack = 1.13 * 3 * U * zg.abs() * zu.abs() + 4 * U * want.abs() + 2.0 ** -20 * (1 + zg.abs()) * want.abs()
+    h = O().gated_ff(q, w, w2, x_scale=qs, gate_scale=ws, up_scale=ws2)
+    assert float(((h.double() - want).abs() - slack - half(BF16) * (want.abs() + slack) - 2.0 ** -125 * (zg * zu).abs()).max()) <= 0.0
