@@ -10,6 +10,7 @@ from . import binding
 _TYPE = {torch.float32: binding.ASD_F32, torch.bfloat16: binding.ASD_BF16, torch.float16: binding.ASD_F16,
          torch.int8: binding.ASD_I8}
 _ACT = {"silu": binding.ASD_ACT_SILU, "gelu": binding.ASD_ACT_GELU}
+_LARGEST = 2 ** 31 - 1   # (sizes are 32-bit integers in the library, and ctypes drops what is above)
 _entries = {}
 
 
@@ -80,6 +81,8 @@ def _out_vector(t, name, dtype, device, n):
 def _rows_of(x, name="x"):
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         _refuse("%s is no matrix" % name)
+    if max(x.shape) > _LARGEST:
+        raise binding.AsdError(binding.ASD_EUNSUPPORTED, "%s has shape %s: up to %d rows and columns" % (name, tuple(x.shape), _LARGEST))
     if x.device.type != "cuda":
         _refuse("%s is on %s, not on a GPU" % (name, x.device))
     return x.shape[0], x.shape[1]
@@ -188,7 +191,7 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, out_type=torch.bfloat16, out=No
             return linear_i8(x, x_scale, w, w_scale, bias, out_type, out, rows_used)
     rows, cols = _rows_of(x)
     dev = x.device
-    channels = w.shape[0] if w.dim() == 2 else 0
+    channels = _rows_of(w, "w")[0]
     if out_type not in _TYPE:
         _refuse("no such type: %s" % out_type)
     a = binding.asd_linear8(rows=rows, cols=cols, channels=channels, out_type=_TYPE[out_type])
@@ -210,7 +213,7 @@ def _gated_args(x, w_gate, w_up, act, out_type):
         _refuse("no such type: %s -> %s" % (t, out_type))
     if act not in _ACT:
         _refuse("unknown activation %r" % (act,))
-    channels = w_gate.shape[0] if w_gate.dim() == 2 else 0
+    channels = _rows_of(w_gate, "w_gate")[0]
     a = binding.asd_gated(rows=rows, cols=cols, channels=channels, type=_TYPE[t], out_type=_TYPE[out_type], act=_ACT[act])
     a.x, a.ld_x = _matrix(x, "x", t, dev, rows, cols)
     a.w_gate, a.ld_w_gate = _matrix(w_gate, "w_gate", t, dev, channels, cols)

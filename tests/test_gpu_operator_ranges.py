@@ -109,3 +109,12 @@ def test_products_of_rows_with_large_scales(rows):
     slack = 1.13 * 3 * U * zg.abs() * zu.abs() + 4 * U * want.abs() + 2.0 ** -20 * (1 + zg.abs()) * want.abs()
     h = O().gated_ff(q, w, w2, x_scale=qs, gate_scale=ws, up_scale=ws2)
     assert float(((h.double() - want).abs() - slack - half(BF16) * (want.abs() + slack) - 2.0 ** -125 * (zg * zu).abs()).max()) <= 0.0
+
+
+def test_channels_that_32_bits_do_not_hold():
+    w = torch.empty((1 << 31) + 5, 1, dtype=torch.int8, device=DEV)
+    x, one = torch.ones(1, 1, dtype=torch.int8, device=DEV), torch.ones(1, device=DEV)
+    for call in (lambda: O().linear_i8(x, one, w, one), lambda: O().gated_ff(x, w, w, x_scale=one, gate_scale=one, up_scale=one)):
+        with pytest.raises(binding.AsdError) as e:
+            call()
+        assert e.value.status == binding.ASD_EUNSUPPORTED

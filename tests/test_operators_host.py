@@ -156,3 +156,16 @@ def test_gated_gradient_workspace_of_a_tall_call():
     n = L.asd_gated_ff_backward_workspace(C.byref(gated(rows=1 << 20, cols=2048, channels=64, ld_x=2048, ld_w_gate=2048, ld_w_up=2048,
                                                         ld_dh=64, ld_dx=2048, ld_dw_gate=2048, ld_dw_up=2048)))
     assert n <= (1 << 20) * 2 * (2048 + 2 * 4 * 64) + (64 << 20)
+
+
+@pytest.mark.parametrize("shape", [(2 ** 31, 8), (2 ** 32 + 3, 8), (8, 2 ** 32 + 16)])
+def test_sizes_that_32_bits_do_not_hold(shape):
+    """Not what is left of them: a call on the first three rows of four billion."""
+    import torch
+    from paper_2505_03983_amd import operators as O
+    x = torch.empty(shape, dtype=torch.bfloat16, device="meta")
+    for call in (lambda: O.quantize_rows(x), lambda: O.rms_norm(x), lambda: O.rms_norm_backward(x, x), lambda: O.gated_ff(x, x, x),
+                 lambda: O.gated_ff_backward(x, x, x, x), lambda: O.linear_i8(x, x[:, 0], x, x[:, 0])):
+        with pytest.raises(b.AsdError) as e:
+            call()
+        assert e.value.status == EUNSUPPORTED
