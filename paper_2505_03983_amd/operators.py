@@ -2,7 +2,9 @@
 outputs and workspaces are allocated by torch, the kernels run on the tensors' device and its current stream.  With `stream` (a
 torch stream of that device) a call is made as under `torch.cuda.stream(stream)`: new outputs are that stream's, and the inputs have
 to be ready for it.  Matrices may have any row pitch; their columns lie next to each other.  Results carry no autograd history: the
-gradients are the *_backward calls.  There is no fallback: without a GPU a call raises."""
+gradients are the *_backward calls, and an argument that requires a gradient is refused where torch would record one (call under
+torch.no_grad(), or from the forward of a torch.autograd.Function, whose backward makes the *_backward call).  There is no fallback:
+without a GPU a call raises."""
 import torch
 
 from . import binding
@@ -25,6 +27,11 @@ def _refuse(message):
     raise binding.AsdError(binding.ASD_EINVAL, message)
 
 
+def _no_history(t, name):
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse("%s requires a gradient, and results carry no autograd history" % name)
+
+
 def _matrix(t, name, dtype, device, rows, cols):
     """Address and row pitch of a matrix argument."""
     if t.shape != (rows, cols):
@@ -33,6 +40,7 @@ def _matrix(t, name, dtype, device, rows, cols):
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
+    _no_history(t, name)
     if t.is_contiguous():
         return t.data_ptr(), cols
     row, col = t.stride()
@@ -54,6 +62,7 @@ def _vector(t, name, dtype, device, n):
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
+    _no_history(t, name)
     if not t.is_contiguous():
         _refuse("the elements of %s do not lie next to each other" % name)
     return t.data_ptr()
