@@ -29,7 +29,7 @@ def device_params(cfg, params, device="cuda:0"):
             if k in params:
                 out[k] = up(params[k])
     for k in ("w_in", "w_blk", "w_out", "b_in", "b_blk", "b_out", "temb"):
-        if k in params:
+        if not (cfg["kind"] == "gated" and k in ("w_blk", "b_blk")):   # (a gated network's blocks are the arrays above)
             out[k] = up(params[k])
     return out
 
