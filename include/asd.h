@@ -293,7 +293,8 @@ ASD_API asd_status asd_denoise(asd_ctx* ctx, const float* x, const int32_t* tau,
  *  - Matrices are row-major; ld_* are elements between rows (>= the row's length).  Rows, sizes and pitches may be odd;
  *    pointers are aligned to their element.  rows may be 0 (nothing is done); other sizes are at least 1.
  *  - All pointers but the structs themselves are DEV, of the device that is current; the call is asynchronous on `stream`,
- *    allocates nothing and may be captured into a graph.  Outputs must not overlap inputs or each other, except where said.
+ *    allocates nothing and may be captured into a graph.  Outputs must not overlap inputs or each other, except where said
+ *    (columns of one wider matrix, at its pitch, do not).
  *  - `workspace` (16-byte aligned, workspace_bytes long; what it holds before does not matter) is the caller's, and one call's
  *    until that call's work on the stream is over: calls on different streams, or graphs that may run at the same time, need
  *    their own.  asd_*_workspace(args) says how many bytes a call with these sizes, types, pitches and pointers needs; 0: none,

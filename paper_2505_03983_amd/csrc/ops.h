@@ -17,6 +17,14 @@ struct MatArg {
   bool out;
   const char* begin() const { return static_cast<const char*>(p); }
   const char* end() const { return begin() + ((rows - 1) * ld + cols) * bytes; }
+  // no byte of the two is the same: one behind the other, or rows of one pitch between each other's (columns of one wider matrix)
+  bool apart(const MatArg& o) const {
+    if (begin() >= o.end() || o.begin() >= end()) return true;
+    const int64_t pitch = ld * bytes;
+    if (rows < 2 || o.rows < 2 || pitch != o.ld * o.bytes) return false;
+    const int64_t at = ((o.begin() - begin()) % pitch + pitch) % pitch;   // where its rows start in this one's
+    return at >= cols * bytes && at + o.cols * o.bytes <= pitch;
+  }
 };
 
 // Pitches, alignment and overlaps of a call's matrices (NULL ones are left out).  may_share(a, b): an output and an input that
@@ -32,7 +40,7 @@ inline asd_status check_mats(const MatArg* m, int n, Share may_share) {
   for (int i = 0; i < n; ++i)
     for (int j = 0; j < n; ++j) {
       if (i == j || !m[i].out || !m[i].p || !m[j].p || m[i].rows < 1 || m[j].rows < 1 || (m[j].out && j < i)) continue;
-      if (m[i].begin() >= m[j].end() || m[j].begin() >= m[i].end()) continue;
+      if (m[i].apart(m[j])) continue;
       if (may_share(i, j) && m[i].p == m[j].p && (m[i].ld == m[j].ld || m[i].rows == 1)) continue;
       return fail(ASD_EINVAL, "%s overlaps %s", m[i].name, m[j].name);
     }

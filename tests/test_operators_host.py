@@ -169,3 +169,27 @@ def test_sizes_that_32_bits_do_not_hold(shape):
         with pytest.raises(b.AsdError) as e:
             call()
         assert e.value.status == EUNSUPPORTED
+
+
+def test_columns_of_one_matrix_are_no_overlap():
+    """Outputs and inputs that are columns of one wider matrix, their rows between each other's, share no byte."""
+    status = lambda call, p: call(C.byref(p), None)   # noqa: E731
+    ld = 256
+    # the shape of a refusal shows where the overlap check ended: with them apart, the next check (no workspace) speaks
+    wide = dict(ld_dw_gate=ld, ld_dw_up=ld, workspace=None, workspace_bytes=0)
+    for off, apart in ((64, True), (192, True), (63, False), (193, False), (1, False), (256 * 5 + 64, True), (0, False)):
+        p = gated(dw_gate=at(10), dw_up=at(10) + 2 * off, **wide)
+        assert status(L.asd_gated_ff_backward, p) == EINVAL
+        assert ("overlaps" not in b.last_error()) == apart, (off, b.last_error())
+    # other pitches, and a row alone
+    p = gated(dw_gate=at(10), dw_up=at(10) + 128, ld_dw_gate=256, ld_dw_up=255, workspace=None, workspace_bytes=0)
+    assert status(L.asd_gated_ff_backward, p) == EINVAL and "overlaps" in b.last_error()
+    p = gated(dx=at(1) + 2 * 128, ld_x=ld, ld_dx=ld, workspace=None, workspace_bytes=0)
+    assert status(L.asd_gated_ff_backward, p) == EINVAL and "overlaps" not in b.last_error()
+    p = gated(dx=at(1) + 2 * 32, ld_x=ld, ld_dx=ld, workspace=None, workspace_bytes=0)
+    assert status(L.asd_gated_ff_backward, p) == EINVAL and "overlaps" in b.last_error()
+    # int8 rows between bf16 ones: pitches in bytes
+    p = norm(x=at(1), ld_x=96, cols=64, out=at(1) + 128, ld_out=192, scale=None)
+    assert status(L.asd_quantize_rows, p) == EINVAL and "scale" in b.last_error()
+    p = norm(x=at(1), ld_x=96, out=at(1) + 127, ld_out=192)
+    assert status(L.asd_quantize_rows, p) == EINVAL and "overlaps" in b.last_error()
