@@ -796,10 +796,14 @@ static asd_status check_workspace(const void* ws, size_t have, size_t need) {
   return ASD_OK;
 }
 
-static asd_status check_linear8(const asd_linear8* p) {
+static asd_status check_linear8_sizes(const asd_linear8* p) {
   if (!p) return fail(ASD_EINVAL, "arguments are NULL");
   ASD_TRY(check_sizes(p->rows, p->cols, p->channels));
   if (p->cols > kMaxI8Cols) return fail(ASD_EUNSUPPORTED, "cols > %d: a sum may leave 32 bits (got %d)", kMaxI8Cols, p->cols);
+  return ASD_OK;
+}
+static asd_status check_linear8(const asd_linear8* p) {
+  ASD_TRY(check_linear8_sizes(p));
   if (!float_type(p->out_type)) return fail(ASD_EINVAL, "unknown out_type %d", p->out_type);
   if (p->rows == 0) return ASD_OK;
   if (!p->x || !p->x_scale || !p->w || !p->w_scale || !p->out) return fail(ASD_EINVAL, "a pointer is NULL");
@@ -815,14 +819,18 @@ static asd_status check_linear8(const asd_linear8* p) {
   return check_workspace(p->workspace, p->workspace_bytes, plan_linear8(*p, nullptr, true).bytes);
 }
 
-static asd_status check_gated(const asd_gated* p, bool backward) {
+static asd_status check_gated_sizes(const asd_gated* p, bool backward) {
   if (!p) return fail(ASD_EINVAL, "arguments are NULL");
   ASD_TRY(check_sizes(p->rows, p->cols, p->channels));
   if (!half_type(p->type) && (backward || p->type != ASD_I8)) return fail(ASD_EINVAL, "type %d is not one of the unit's", p->type);
   if (!half_type(p->type) && p->cols > kMaxI8Cols) return fail(ASD_EUNSUPPORTED, "cols > %d: a sum may leave 32 bits (got %d)", kMaxI8Cols, p->cols);
   if (p->cols > kMaxCols) return fail(ASD_EUNSUPPORTED, "cols > %d (got %d)", kMaxCols, p->cols);
-  if (p->act != ASD_ACT_SILU && p->act != ASD_ACT_GELU) return fail(ASD_EINVAL, "unknown activation %d", p->act);
   if (backward && (p->rows > kMaxCols || p->channels > kMaxCols)) return fail(ASD_EUNSUPPORTED, "gradients: rows and channels up to %d", kMaxCols);
+  return ASD_OK;
+}
+static asd_status check_gated(const asd_gated* p, bool backward) {
+  ASD_TRY(check_gated_sizes(p, backward));
+  if (p->act != ASD_ACT_SILU && p->act != ASD_ACT_GELU) return fail(ASD_EINVAL, "unknown activation %d", p->act);
   if (backward && p->rows_used) return fail(ASD_EINVAL, "gradients take no rows_used");
   if (backward && (p->dw_gate != nullptr) != (p->dw_up != nullptr)) return fail(ASD_EINVAL, "dw_gate and dw_up go together");
   if (!backward && (p->type == ASD_I8 ? !half_type(p->out_type) : p->out_type != p->type))
@@ -863,8 +871,9 @@ using namespace asd;
 
 extern "C" {
 
+// (sizes that the call refuses need nothing: it says so itself, where an allocation for them would fail first)
 size_t asd_linear_i8_workspace(const asd_linear8* p) {
-  return !p || p->rows < 1 || p->cols < 1 || p->channels < 1 ? 0 : plan_linear8(*p, nullptr, true).bytes;
+  return check_linear8_sizes(p) != ASD_OK || p->rows == 0 ? 0 : plan_linear8(*p, nullptr, true).bytes;
 }
 
 asd_status asd_linear_i8(const asd_linear8* p, void* stream) {
@@ -873,7 +882,7 @@ asd_status asd_linear_i8(const asd_linear8* p, void* stream) {
 }
 
 size_t asd_gated_ff_workspace(const asd_gated* p) {
-  if (!p || p->rows < 1 || p->cols < 1 || p->channels < 1) return 0;
+  if (check_gated_sizes(p, false) != ASD_OK || p->rows == 0) return 0;
   Carve c{nullptr};
   return plan_gated(*p, &c).bytes;
 }
@@ -884,7 +893,7 @@ asd_status asd_gated_ff(const asd_gated* p, void* stream) {
 }
 
 size_t asd_gated_ff_backward_workspace(const asd_gated* p) {
-  if (!p || p->rows < 1 || p->cols < 1 || p->channels < 1) return 0;
+  if (check_gated_sizes(p, true) != ASD_OK || p->rows == 0) return 0;
   asd_gated q = *p;
   q.workspace = nullptr;
   return plan_gated_grad(q).bytes;

@@ -480,7 +480,7 @@ asd_status asd_quantize_rows(const asd_norm* p, void* stream) {
 }
 
 size_t asd_rms_norm_backward_workspace(const asd_norm_grad* p) {
-  if (!p || !p->dgain || p->rows < 1 || p->cols < 1) return 0;
+  if (!p || !p->dgain || check_norm_sizes(p->rows, p->cols, p->type) != ASD_OK || p->rows == 0) return 0;
   return sizeof(float) * (size_t)norm_grad_parts(p->rows, p->cols) * (size_t)p->cols;
 }
 

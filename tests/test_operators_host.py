@@ -193,3 +193,21 @@ def test_columns_of_one_matrix_are_no_overlap():
     assert status(L.asd_quantize_rows, p) == EINVAL and "scale" in b.last_error()
     p = norm(x=at(1), ld_x=96, out=at(1) + 127, ld_out=192)
     assert status(L.asd_quantize_rows, p) == EINVAL and "overlaps" in b.last_error()
+
+
+def test_sizes_that_are_refused_need_no_workspace():
+    """The refusal is the call's, not that of an allocation for it."""
+    wide = dict(ld_x=1 << 21, ld_w_gate=1 << 21, ld_w_up=1 << 21, ld_dh=1 << 21, ld_dx=1 << 21, ld_dw_gate=1 << 21, ld_dw_up=1 << 21)
+    for kw in (dict(rows=(1 << 20) + 1), dict(channels=(1 << 20) + 1), dict(cols=(1 << 20) + 8), dict(type=b.ASD_F32), dict(rows=-5),
+               dict(channels=2 ** 31 - 1)):
+        p = gated(**{**wide, **kw})
+        assert L.asd_gated_ff_backward_workspace(C.byref(p)) == 0, kw
+        p.workspace, p.workspace_bytes = None, 0
+        assert L.asd_gated_ff_backward(C.byref(p), None) in (EINVAL, EUNSUPPORTED) and "workspace" not in b.last_error()
+    assert L.asd_gated_ff_workspace(C.byref(gated(cols=(1 << 20) + 8, x=at(1) + 2))) == 0
+    assert L.asd_gated_ff_workspace(C.byref(gated(rows=(1 << 28) + 1, x=at(1) + 2))) == 0
+    assert L.asd_linear_i8_workspace(C.byref(linear(cols=131073, ld_x=131073, ld_w=131073))) == 0
+    assert L.asd_linear_i8_workspace(C.byref(linear(rows=-1, ld_x=65))) == 0
+    assert L.asd_rms_norm_backward_workspace(C.byref(grad(cols=32769))) == 0
+    # ... and the largest that are taken say what they need
+    assert L.asd_gated_ff_backward_workspace(C.byref(gated(rows=1 << 20))) > 0 and L.asd_linear_i8_workspace(C.byref(linear(cols=131071))) > 0
