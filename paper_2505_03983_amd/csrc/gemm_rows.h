@@ -621,13 +621,15 @@ __global__ __launch_bounds__(512) void gemm_rows_big_kernel(RowsProduct p, int t
 // 64 bytes of 16 rows), DEPTH such pieces in flight, and the eight partial sums meet in LDS.  Sums are added in the order of
 // the wavefronts: the same bits every time, and for any number of rows.  Plain loads: marked as not to be kept, the weights of a
 // network that the Infinity Cache holds came from memory every time (67 MB of 8-bit gated weights, one row, 15.5 -> 13.0 us).
+constexpr int kFewGrid = 65536;
 template <class E, int MT, class Epi>
 __global__ __launch_bounds__(512) void gemm_few_rows_kernel(RowsProduct p, Epi epi) {
   constexpr bool GATED = Epi::kGated;
   constexpr int WT = GATED ? 2 : 1, NWAVES = 8, DEPTH = MT == 1 ? 4 : 2;
   const int M = p.rows_used ? min(max(*p.rows_used, 0), p.M) : p.M;
-  // (channels over two dimensions of the grid: 2^28 of them are more than 2^32 threads)
-  const int m0 = blockIdx.z * (16 * MT), n0 = (int)(blockIdx.y * gridDim.x + blockIdx.x) * 16;
+  // (channels over two dimensions of the grid, 2^28 of them being more than 2^32 threads, in rows of kFewGrid workgroups: gridDim.x
+  // is a load from memory)
+  const int m0 = blockIdx.z * (16 * MT), n0 = (int)(blockIdx.y * kFewGrid + blockIdx.x) * 16;
   if (m0 >= M || n0 >= epi.columns()) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
   const uint8_t* wrow[WT];

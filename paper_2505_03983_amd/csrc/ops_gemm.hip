@@ -527,8 +527,8 @@ static Split pick_split(int M, int64_t n, int64_t kb) {
 
 template <class E, int MT, class Epi>
 static hipError_t launch_few(const RowsProduct& p, const Epi& e, hipStream_t st) {
-  dim3 grid = grid_of(ceil_div(e.columns(), 16));
-  grid.z = (unsigned)ceil_div(p.M, 16 * MT);
+  const int64_t wgs = ceil_div(e.columns(), 16);
+  const dim3 grid((unsigned)std::min<int64_t>(wgs, kFewGrid), (unsigned)ceil_div(wgs, kFewGrid), (unsigned)ceil_div(p.M, 16 * MT));
   hipLaunchKernelGGL((gemm_few_rows_kernel<E, MT, Epi>), grid, dim3(512), 0, st, p, e);
   return hipGetLastError();
 }

@@ -27,11 +27,6 @@ def _refuse(message):
     raise binding.AsdError(binding.ASD_EINVAL, message)
 
 
-def _no_history(t, name):
-    if t.requires_grad and torch.is_grad_enabled():
-        _refuse("%s requires a gradient, and results carry no autograd history" % name)
-
-
 def _matrix(t, name, dtype, device, rows, cols):
     """Address and row pitch of a matrix argument."""
     if t.shape != (rows, cols):
@@ -40,7 +35,8 @@ def _matrix(t, name, dtype, device, rows, cols):
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
-    _no_history(t, name)
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse("%s requires a gradient, and results carry no autograd history" % name)
     if t.is_contiguous():
         return t.data_ptr(), cols
     row, col = t.stride()
@@ -62,7 +58,8 @@ def _vector(t, name, dtype, device, n):
         _refuse("%s is %s, not %s" % (name, t.dtype, dtype))
     if t.device != device:
         _refuse("%s is on %s, not on %s" % (name, t.device, device))
-    _no_history(t, name)
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse("%s requires a gradient, and results carry no autograd history" % name)
     if not t.is_contiguous():
         _refuse("the elements of %s do not lie next to each other" % name)
     return t.data_ptr()
@@ -90,11 +87,12 @@ def _out_vector(t, name, dtype, device, n):
 def _rows_of(x, name="x"):
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         _refuse("%s is no matrix" % name)
-    if max(x.shape) > _LARGEST:
+    rows, cols = x.shape
+    if rows > _LARGEST or cols > _LARGEST:
         raise binding.AsdError(binding.ASD_EUNSUPPORTED, "%s has shape %s: up to %d rows and columns" % (name, tuple(x.shape), _LARGEST))
     if x.device.type != "cuda":
         _refuse("%s is on %s, not on a GPU" % (name, x.device))
-    return x.shape[0], x.shape[1]
+    return rows, cols
 
 
 def _on(stream, device):
