@@ -107,7 +107,7 @@ struct RowScale {
   float s, up;
 };
 __device__ __forceinline__ RowScale row_scale(float v) {
-  return v > 0x1p96f ? RowScale{v * 0x1p-32f, 0x1p32f} : RowScale{v, 1.f};
+  return fabsf(v) > 0x1p96f ? RowScale{v * 0x1p-32f, 0x1p32f} : RowScale{v, 1.f};
 }
 
 // out = sum x_scale w_scale + bias

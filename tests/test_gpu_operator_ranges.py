@@ -88,12 +88,14 @@ def test_norm_gradient_of_more_rows_than_threads_in_a_dimension():
     assert float(dx.float().abs().max()) == 0.0
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
 @pytest.mark.parametrize("rows", [1, 40, 300, 2000])
-def test_products_of_rows_with_large_scales(rows):
+def test_products_of_rows_with_large_scales(rows, sign):
     """Rows next to fp32's largest number, weights as small as that: the sum times one scale leaves fp32, times both it does not."""
     g = torch.Generator(device=DEV).manual_seed(rows)
     cols, channels = 272, 2100
     q, qs = O().quantize_rows(randn(g, rows, cols).clamp(-3, 3) * 1e38)
+    qs = qs * sign
     w, ws = O().quantize_rows(randn(g, channels, cols) * 1e-36)
     w2, ws2 = O().quantize_rows(randn(g, channels, cols) * 1e-36)
     assert bool(torch.isfinite(qs).all()) and bool(torch.isinf((q.float() @ w.float().T).abs() * qs[:, None]).any())
