@@ -450,7 +450,7 @@ __global__ __launch_bounds__(Cfg::THREADS) void gemm_rows_kernel(RowsProduct p, 
 // product, and this kernel is where the chip's power is the limit (1.5 GHz on random operands, 2.4 on zeros): 8192 x 32768 x 4096
 // in bf16 1703 us for 1800, and 1885 with the pipeline above.  (A workgroup that takes one tile after the other, the next one's
 // first stages under the results of the last, saves 2 us of a tile's 10 of fill and drain and loses 0.07 of each of its stages' 1.13: 7.09
-// ms for 7.00 of a training step.)
+// ms for 7.00 of a training step, dg and du being one number each.)
 typedef RowsCfg<256, 256, 2, 4, 128, 2> Rows256;
 
 template <class E, class Epi>
