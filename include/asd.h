@@ -375,7 +375,7 @@ ASD_API asd_status asd_linear_i8(const asd_linear8* p, void* stream);
  *   type ASD_I8: g and u as asd_linear_i8 has them, without bias; out_type ASD_BF16 or ASD_F16; cols <= 131071.
  * asd_gated_ff_backward: from dh [rows, channels], the gradient of out (ASD_BF16, ASD_F16; pitch ld_dh), with
  *   dg = dh u act'(g), du = dh act(g) (g, u computed again, in fp32; dg, du enter the products as the sum of two bf16 numbers,
- *   fp16 operands as two as well: nothing is lost where dg, du leave fp16's range):
+ *   fp16 operands as two as well: nothing is lost where dg, du leave fp16's range; an infinite one may come out as NaN):
  *   dx = dg W_gate + du W_up [rows, cols],  dw_gate = dg^T x,  dw_up = du^T x [channels, cols], all in `type`.  dx may be NULL,
  *   and dw_gate and dw_up may both be.  rows 0: the weights' gradients are zero.  rows_used must be NULL. */
 typedef struct {
